@@ -50,7 +50,8 @@ typedef enum {
     ATTN_ERR_ALIGNMENT = -3,      /* a base pointer is not 16-byte aligned */
     ATTN_ERR_NO_DEVICE = -4,      /* no usable CUDA device / driver */
     ATTN_ERR_CUDA = -5,           /* a CUDA runtime or driver call failed */
-    ATTN_ERR_DEVICE_TIMEOUT = -6  /* a bounded wait inside the kernel ran out (see attn_device_status) */
+    ATTN_ERR_DEVICE_TIMEOUT = -6, /* a bounded wait inside the kernel ran out (see attn_device_status) */
+    ATTN_ERR_INDEX = -7           /* a kernel met a length, page or slot out of range (see attn_device_status) */
 } attn_status;
 
 typedef enum { ATTN_SCAN_CYCLIC = 0, ATTN_SCAN_SAWTOOTH = 1 } attn_scan_order;
@@ -242,10 +243,131 @@ int attn_dynamic_claim_trace(int B, int H, int N, int d, int causal, int scan_or
                              const attn_fwd_opts* opts, int sm_count,
                              attn_trace_entry* buf, size_t cap, size_t* n);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Around the attention kernel in a server (outside the paper): keys and values kept in pages, the tables that say which
+ * page holds what, and the step that puts new keys and values there.
+ * A step is: attn_page_plan (once for all layers), then per layer attn_qk_norm_rope on the projections.  All of it can be captured into a CUDA graph: lengths,
+ * tables and the pool of free pages live on the device.
+ *
+ * A device's first call of an entry point looks symbols up and raises limits (make it outside any stream capture);
+ * later ones only enqueue work on `stream`.  No entry point waits unless its options say check_mode.
+ */
+
+/*
+ * Keys and values of one layer in pages of page_size tokens.  layout: ATTN_LAYOUT_BNHD = [page, token, kv_head, d]
+ * or ATTN_LAYOUT_BHND = [page, kv_head, token, d]; the three strides, in elements, are those of k and of v alike, all
+ * three 0 for contiguous arrays (then K and V may still be two halves of one array: give the strides).  Strides are multiples
+ * of 8 and k and v 16-byte aligned.  Slot s of the cache is token s % page_size of page s / page_size.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    long long num_pages;
+    long long page_stride, token_stride, head_stride;
+    int page_size;   /* 1 .. 65536, any number */
+    int kv_heads;
+    int d;           /* 64 or 128 */
+    int dtype;       /* attn_dtype */
+    int layout;      /* attn_layout; looked at only when the strides are 0 */
+    int reserved[3];
+} attn_kv_cache;
+
+/*
+ * Block tables, slot maps and positions of a step, on the GPU.  Request b has cached[b] tokens in its pages,
+ * block_table[b * table_stride + i] being its i-th page, and
+ *   added[b] >= 0  takes that many more tokens (zero is fine): new pages come from the pool as needed, in the order of requests
+ *                  and within a request of pages, always the one on top of the stack;
+ *   added[b] = -1  ends: all its pages go back onto the stack (in the order of requests and of their tables) before any
+ *                  is taken.  Its row of the table is left as it was.
+ * The pool is a stack: free_pages[0 .. count-1], the top last, in an array of `capacity` entries.
+ *
+ * seq_len[b] = cached[b] + added[b] (0 for a request that ended); it may be the array `cached` itself.  The new tokens
+ * are numbered request after request: q_start[b] is request b's first, q_start[B] their count T.  For token t of request b:
+ * position[t] = cached[b] + t - q_start[b], slot[t] = the cache slot of that position, request[t] = b.  For T <= t <
+ * token_cap: slot -1, position 0, request -1, so that a captured graph can run a fixed number of rows.  position and request may be NULL.
+ * free_count_out may be free_count itself.
+ *
+ * info[0] says whether the step fits; if not, nothing is taken, the table and the pool stay as they are, seq_len = cached
+ * (entries as given), free_count_out = free_count, q_start is 0 throughout and all slots are -1.  info[1] = T, info[2] = pages taken,
+ * info[3] = pages given back (of a step that does not fit: what it would have needed, 0 where the lengths are bad).
+ *
+ * 1 <= B <= 8192; width * page_size and B * width below 2^31.  Arrays other than the two pairs named above must not overlap.
+ */
+typedef enum {
+    ATTN_PLAN_FITS = 0,
+    ATTN_PLAN_BAD_LENGTH = 1,   /* a length below 0, above the table's width, or added below -1; a count outside [0, capacity] */
+    ATTN_PLAN_NO_ROOM = 2,      /* T exceeds token_cap */
+    ATTN_PLAN_NO_PAGES = 3      /* too few free pages, or more given back than the pool can hold */
+} attn_plan_state;
+
+typedef struct {
+    int* block_table;        /* [B, width], rows table_stride entries apart */
+    long long table_stride;
+    int* free_pages;         /* [capacity] */
+    const int* free_count;   /* [1] */
+    int* free_count_out;     /* [1] */
+    int width;               /* pages a request can have */
+    int capacity;
+    int page_size;           /* 1 .. 65536 */
+    int reserved;
+} attn_page_pool;
+
+int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* added, int B, int* seq_len, int* q_start, long long* slot,
+                   int* position, int* request, int token_cap, int* info, void* stream);
+
+/*
+ * RMS norm of every query and key head, the position rotation, and the append of keys and values to the cache, in one pass.
+ * For every token t and head, with x the head's d values and w the weight (q_weight or k_weight, shared by all heads):
+ *     n = x * w / sqrt(mean(x^2) + eps)              (n = x where the weight is NULL)
+ *     (a, b) -> (a cos f - b sin f, b cos f + a sin f),   f = position[t] * inv_freq[i]
+ * for the pairs i < rot_dim / 2 of the first rot_dim values: (n[i], n[i + rot_dim/2]) in the style ATTN_ROPE_HALVES,
+ * (n[2i], n[2i+1]) in ATTN_ROPE_ADJACENT; the others stay.  Angles are reduced in 64 bits, everything else is computed in 32
+ * bits, and each result is rounded once.
+ *
+ * q [T, H, d], k and v [T, kv_heads, d], q_out and k_out like q and k: rows of d contiguous elements at a token and a head
+ * stride (opts; 0 = contiguous), so q, k and v may be parts of one projection's output.  q_out may be q and k_out may be k
+ * (same strides); otherwise outputs overlap nothing.  With opts->cache, k's results and v are written to the cache at slot[t]; a row with
+ * slot[t] < 0 (padding) is left alone altogether, q_out and k_out included; a slot beyond the cache is not written and noted in
+ * the status word.  Two rows must not share a slot.  k_out may be NULL when there is a cache; v is needed exactly then.
+ * rot_dim: 0 (no rotation; position and inv_freq may be NULL) or a multiple of 16 up to d.  T may be 0.  Weights: of `dtype`,
+ * or fp32 (opts->weight_f32).  Base pointers 16-byte aligned, strides multiples of 8 elements.
+ */
+typedef enum { ATTN_ROPE_HALVES = 0, ATTN_ROPE_ADJACENT = 1 } attn_rope_style;
+
+typedef struct {
+    /* token and head strides in elements; both 0 = contiguous [T, heads, d] */
+    long long q_token, q_head, k_token, k_head, v_token, v_head;
+    long long q_out_token, q_out_head, k_out_token, k_out_head;   /* of the backward pass: dq_out and dk_out */
+    long long dq_token, dq_head, dk_token, dk_head;               /* backward pass only: dq and dk */
+    const attn_kv_cache* cache;   /* forward pass only */
+    const long long* slot;        /* [T], with cache */
+    int weight_f32;               /* 1: the weights are fp32 */
+    int check_mode;               /* as in attn_fwd_opts */
+    int reserved[2];
+} attn_rope_opts;
+
+int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out, int T, int H, int kv_heads, int d, int dtype,
+                      const void* q_weight, const void* k_weight, float eps, const int* position, const double* inv_freq, int rot_dim,
+                      int rot_style, void* stream, const attn_rope_opts* opts);
+
+/*
+ * Gradients of the above.  Given dq_out, dk_out (gradients of q_out, k_out) and the forward pass's inputs q, k: with R^T the
+ * rotation back, r = 1 / sqrt(mean(x^2) + eps), dn = R^T dy,
+ *     dx = r * (dn w - x r^2 mean(dn w x)),   dw = sum over tokens and heads of dn x r     (dx = dn without a weight).
+ * dq may be dq_out and dk may be dk_out (same strides).  dq_weight, dk_weight: [d] fp32, overwritten; NULL exactly where the weight is.
+ * For fixed arguments bitwise reproducible.  workspace: attn_rope_bwd_workspace_bytes(d) bytes, 16-byte aligned, contents of no
+ * matter; calls that share one must not overlap on the GPU.
+ */
+size_t attn_rope_bwd_workspace_bytes(int d);
+int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, void* dq, void* dk, float* dq_weight,
+                          float* dk_weight, int T, int H, int kv_heads, int d, int dtype, const void* q_weight, const void* k_weight,
+                          float eps, const int* position, const double* inv_freq, int rot_dim, int rot_style, void* workspace,
+                          size_t workspace_bytes, void* stream, const attn_rope_opts* opts);
+
 /*
  * Waits for the current device and reads, then clears, its kernel status word: 0, or a code naming
- * the wait that ran out in a kernel launched since the last call.  Returns ATTN_OK when the word
- * was 0, ATTN_ERR_DEVICE_TIMEOUT otherwise (code in *code if code != NULL).
+ * the wait that ran out, or the index that was out of range, in a kernel launched since the last call.  Returns ATTN_OK
+ * when the word was 0, ATTN_ERR_DEVICE_TIMEOUT or ATTN_ERR_INDEX otherwise (code in *code if code != NULL).
  */
 int attn_device_status(int* code);
 

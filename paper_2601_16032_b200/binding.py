@@ -10,6 +10,8 @@ F16, BF16 = 0, 1
 TILE_FASTEST, HEAD_FASTEST = 0, 1
 PAIR_DEFAULT, PAIR_NONE, PAIR_MIRRORED, PAIR_ADJACENT = 0, 1, 2, 3
 LAYOUT_BHND, LAYOUT_BNHD = 0, 1
+ROPE_HALVES, ROPE_ADJACENT = 0, 1
+PLAN_FITS, PLAN_BAD_LENGTH, PLAN_NO_ROOM, PLAN_NO_PAGES = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libsawtooth_attn.so")
@@ -50,6 +52,35 @@ class TraceEntry(ctypes.Structure):
     ]
 
 
+class KVCache(ctypes.Structure):
+    """attn_kv_cache: keys and values in pages; strides in elements (all three 0: contiguous in `layout`)."""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_pages", ctypes.c_longlong),
+        ("page_stride", ctypes.c_longlong), ("token_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+        ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("layout", ctypes.c_int),
+        ("reserved", ctypes.c_int * 3),
+    ]
+
+
+class PagePool(ctypes.Structure):
+    """attn_page_pool: the block tables and the stack of free pages."""
+    _fields_ = [
+        ("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_longlong), ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+        ("free_count_out", ctypes.c_void_p), ("width", ctypes.c_int), ("capacity", ctypes.c_int), ("page_size", ctypes.c_int),
+        ("reserved", ctypes.c_int),
+    ]
+
+
+class RopeOpts(ctypes.Structure):
+    """attn_rope_opts: strides in elements (a pair of zeros: contiguous), the cache and slots of the forward pass."""
+    _fields_ = [(name, ctypes.c_longlong) for name in (
+        "q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "q_out_token", "q_out_head", "k_out_token", "k_out_head",
+        "dq_token", "dq_head", "dk_token", "dk_head")] + [
+        ("cache", ctypes.POINTER(KVCache)), ("slot", ctypes.c_void_p), ("weight_f32", ctypes.c_int), ("check_mode", ctypes.c_int),
+        ("reserved", ctypes.c_int * 2),
+    ]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -83,6 +114,13 @@ def load_library():
     lib.attn_device_status.argtypes = [ctypes.POINTER(ci)]
     lib.attn_last_kernel_cycles.argtypes = [ctypes.POINTER(ctypes.c_ulonglong)]
     lib.attn_last_kernel_cycles.restype = ci
+    lib.attn_page_plan.argtypes = [ctypes.POINTER(PagePool), vp, vp, ci, vp, vp, vp, vp, vp, ci, vp, vp]
+    lib.attn_qk_norm_rope.argtypes = [vp] * 5 + [ci] * 5 + [vp, vp, cf, vp, vp, ci, ci, vp, ctypes.POINTER(RopeOpts)]
+    lib.attn_rope_bwd_workspace_bytes.argtypes = [ci]
+    lib.attn_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [ci] * 5 + [vp, vp, cf, vp, vp, ci, ci, vp, ctypes.c_size_t, vp, ctypes.POINTER(RopeOpts)]
+    for name in ("attn_page_plan", "attn_qk_norm_rope", "attn_qk_norm_rope_bwd"):
+        getattr(lib, name).restype = ci
     for name in ("attn_fwd", "attn_fwd_ex", "attn_fwd_host", "attn_query_plan", "attn_schedule_trace", "attn_device_status"):
         getattr(lib, name).restype = ci
     lib.attn_status_string.argtypes = [ci]
@@ -184,8 +222,33 @@ def attn_host_groups(heads: int, head_bytes: int, host_chunks: int = 0) -> list:
     return [int(sizes[i]) for i in range(n.value)]
 
 
+def attn_page_plan(pool: PagePool, cached: int, added: int, B: int, seq_len: int, q_start: int, slot: int, position: int, request: int,
+                   token_cap: int, info: int, stream: int = 0) -> None:
+    """Block tables, slots and positions of a step; all arrays are device addresses (position, request: 0 for none)."""
+    _check(load_library().attn_page_plan(ctypes.byref(pool), cached, added, B, seq_len, q_start, slot, position, request, token_cap, info, stream))
+
+
+def attn_qk_norm_rope(q: int, k: int, v: int, q_out: int, k_out: int, T: int, H: int, kv_heads: int, d: int, dtype: int, q_weight: int,
+                      k_weight: int, eps: float, position: int, inv_freq: int, rot_dim: int, rot_style: int, stream: int = 0,
+                      opts: Optional[RopeOpts] = None) -> None:
+    _check(load_library().attn_qk_norm_rope(q, k, v, q_out, k_out, T, H, kv_heads, d, dtype, q_weight, k_weight, eps, position, inv_freq,
+                                            rot_dim, rot_style, stream, _opts_ptr(opts)))
+
+
+def attn_rope_bwd_workspace_bytes(d: int) -> int:
+    return int(load_library().attn_rope_bwd_workspace_bytes(d))
+
+
+def attn_qk_norm_rope_bwd(dq_out: int, dk_out: int, q: int, k: int, dq: int, dk: int, dq_weight: int, dk_weight: int, T: int, H: int, kv_heads: int,
+                          d: int, dtype: int, q_weight: int, k_weight: int, eps: float, position: int, inv_freq: int, rot_dim: int, rot_style: int,
+                          workspace: int, workspace_bytes: int, stream: int = 0, opts: Optional[RopeOpts] = None) -> None:
+    _check(load_library().attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, dq_weight, dk_weight, T, H, kv_heads, d, dtype, q_weight, k_weight, eps,
+                                                position, inv_freq, rot_dim, rot_style, workspace, workspace_bytes, stream, _opts_ptr(opts)))
+
+
 def attn_device_status() -> int:
-    """Synchronises the device; returns 0, or raises AttnError if a kernel wait ran out since the last call."""
+    """Synchronises the device; returns 0, or raises AttnError if a kernel wait ran out, or a kernel met an index out of range,
+    since the last call."""
     code = ctypes.c_int(0)
     _check(load_library().attn_device_status(ctypes.byref(code)))
     return code.value

@@ -8,15 +8,25 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libsawtooth_attn.so")
-SOURCES = [os.path.join(CSRC, "api.cu")]
-DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("attn_fwd_sm100.cuh", "ptx.cuh", "schedule.h")] + \
-    [os.path.join(ROOT, "include", "sawtooth_attn.h")]
+OBJ = os.path.join(PKG, "_build")
+_HEADER = os.path.join(ROOT, "include", "sawtooth_attn.h")
+# Each source with the headers it includes (it is compiled again when one of them is newer than its object file).
+SOURCES = {
+    "api.cu": ("attn_fwd_sm100.cuh", "ptx.cuh", "schedule.h", "host.h"),
+    "paged.cu": ("ptx.cuh", "host.h", "paged_common.cuh", "page_plan.cuh", "qk_norm_rope.cuh"),
+}
+
+
+def _deps(source: str) -> list:
+    return [os.path.join(CSRC, f) for f in (source,) + SOURCES[source]] + [_HEADER]
+
+
+DEPS = sorted({f for source in SOURCES for f in _deps(source)})
 
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-shared",
-    "-cudart", "static",
+    "-Xcompiler", "-fPIC",
 ]
 
 
@@ -28,11 +38,25 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Compiles the sources that changed (side by side) and links the library."""
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + SOURCES
-    subprocess.run(cmd, check=True)
+    os.makedirs(OBJ, exist_ok=True)
+    running, objects = [], []
+    for source in SOURCES:
+        obj = os.path.join(OBJ, source[:-3] + ".o")
+        objects.append(obj)
+        if force or not os.path.exists(obj) or any(os.path.getmtime(f) > os.path.getmtime(obj) for f in _deps(source)):
+            cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj, os.path.join(CSRC, source)]
+            running.append((cmd, obj, subprocess.Popen(cmd)))
+    failed = [(cmd, obj, p.returncode) for cmd, obj, p in running if p.wait() != 0]
+    if failed:
+        for _, obj, _ in failed:
+            if os.path.exists(obj):
+                os.remove(obj)
+        raise subprocess.CalledProcessError(failed[0][2], failed[0][0])
+    subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static", "-o", LIB] + objects, check=True)
     return LIB
 
 

@@ -10,13 +10,13 @@
 
 #include "../../include/sawtooth_attn.h"
 #include "attn_fwd_sm100.cuh"
+#include "host.h"
 
 namespace {
-
-using namespace sawtooth;
-
 thread_local char g_error[512] = "";
+}
 
+namespace sawtooth {
 int fail(int status, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
@@ -24,6 +24,11 @@ int fail(int status, const char* fmt, ...) {
     va_end(ap);
     return status;
 }
+}  // namespace sawtooth
+
+namespace {
+
+using namespace sawtooth;
 
 __device__ int g_status_word = 0;
 __device__ unsigned long long g_cycles = 0;
@@ -32,22 +37,10 @@ __device__ unsigned long long g_cycles = 0;
 // that loads the library for as long as the process lives.
 static __device__ __align__(256) int g_noalloc_scratch[(ATTN_DYNAMIC_SCRATCH_HEADER / 4) + ATTN_NOALLOC_MAX_CTAS];
 
-constexpr int kMaxDevices = 64;
 constexpr int kMaxHostChunks = 32;
 constexpr int kSmemOptinB200 = 232448;  // 227 KiB of dynamic shared memory per CTA on sm_100
 constexpr int kKernelVariants = 16;     // d x block_n x q_tiles x dtype
 
-// What the library knows about a device, looked up once (under the mutex) on the first call that has it current:
-// its size, the device addresses of the library's own __device__ variables there, and which kernel variants have had
-// their dynamic shared memory limit raised.  Readers take a copy under the same mutex.
-struct DeviceState {
-    bool ready = false;
-    int sm_count = 0, smem_optin = 0;
-    int* status = nullptr;
-    unsigned long long* cycles = nullptr;
-    int* noalloc_scratch = nullptr;
-    unsigned smem_raised = 0;   // bit v: variant v of the kernel may use smem_optin bytes
-};
 DeviceState g_device[kMaxDevices];
 std::mutex g_device_mutex;
 
@@ -116,7 +109,9 @@ int resolve_opts(const attn_fwd_opts* o, int d, int H, int causal, bool dynamic,
     return ATTN_OK;
 }
 
-// The current device's entry of g_device, filled on first use.  *dev_out gets the device index.
+}  // namespace
+
+namespace sawtooth {
 int current_device(DeviceState* out, int* dev_out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -146,6 +141,18 @@ int current_device(DeviceState* out, int* dev_out) {
     if (dev_out) *dev_out = dev;
     return ATTN_OK;
 }
+
+int raise_smem(int dev, const DeviceState& ds, const void* kernel, int bit, int bytes) {
+    if (ds.paged_raised & (1u << bit)) return ATTN_OK;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) { cudaGetLastError(); return fail(ATTN_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e)); }
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    g_device[dev].paged_raised |= 1u << bit;
+    return ATTN_OK;
+}
+}  // namespace sawtooth
+
+namespace {
 
 // n_units: work items, or pairs of them (what one trip of a CTA's loop handles).
 int grid_for(long long n_units, int sm_count, const Resolved& r) {
@@ -263,7 +270,9 @@ int launch_tiles(int block_n, int q_tiles, int dtype, int dev, const DeviceState
                         : launch_dtype<kD, 64, 1>(dtype, dev, ds, m, kp, grid, smem, stream);
 }
 
-// Reads and clears the current device's status word after a device synchronisation.
+}  // namespace
+
+namespace sawtooth {
 int read_status(int* code) {
     cudaError_t e = cudaDeviceSynchronize();
     if (e != cudaSuccess) { cudaGetLastError(); return fail(ATTN_ERR_CUDA, "cudaDeviceSynchronize: %s", cudaGetErrorString(e)); }
@@ -274,12 +283,14 @@ int read_status(int* code) {
     if (word != 0) {
         const int zero = 0;
         cudaMemcpyToSymbol(g_status_word, &zero, sizeof(int));
+        if (word >= kFirstIndexCode)
+            return fail(ATTN_ERR_INDEX, "a kernel met %s out of range (code %d)",
+                        word == kIndexLength ? "a sequence length" : word == kIndexPage ? "a page number" : "a slot", word);
         return fail(ATTN_ERR_DEVICE_TIMEOUT, "kernel wait site %d ran out of time", word);
     }
     return ATTN_OK;
 }
-
-}  // namespace
+}  // namespace sawtooth
 
 extern "C" {
 
@@ -292,6 +303,7 @@ const char* attn_status_string(int status) {
         case ATTN_ERR_NO_DEVICE: return "no CUDA device";
         case ATTN_ERR_CUDA: return "CUDA call failed";
         case ATTN_ERR_DEVICE_TIMEOUT: return "a bounded wait inside the kernel ran out";
+        case ATTN_ERR_INDEX: return "a kernel met a length, page or slot out of range";
         default: return "unknown status";
     }
 }

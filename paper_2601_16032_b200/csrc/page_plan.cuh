@@ -1,0 +1,166 @@
+// Block tables, slot maps and positions of a serving step from the requests' lengths: one cluster of CTAs.
+//
+// Per request: tokens added, pages taken, pages given back; their prefix sums over the requests say where each token, taken
+// and returned page stands.  Every CTA of the cluster makes the (short) scan for itself and keeps it in shared memory; after
+// a cluster barrier, behind which no input is read that an output may alias, the threads of all CTAs together write one
+// token or one page each, finding its request by bisection.
+//
+// With c free pages and R returned ones the stack is free[0 .. c-1], returned[0 .. R-1]; the i-th page taken is entry c + R - 1 - i.
+// Entries below c come from the array, the others from the tables of the requests that end, and what stays on the stack of the
+// returned ones is written to free[c ..]: the entries read and those written are disjoint, so no order among threads is needed.
+#pragma once
+#include "paged_common.cuh"
+
+namespace sawtooth {
+
+constexpr int kPlanMaxRequests = 8192;
+
+struct PagePlanParams {
+    const int* cached;
+    const int* added;
+    int* table;
+    long long table_stride;
+    int* free_pages;
+    const int* free_count;
+    int* free_count_out;
+    int* seq_len;
+    int* q_start;
+    long long* slot;
+    int* position;   // or nullptr
+    int* request;    // or nullptr
+    int* info;
+    int B, width, capacity, token_cap;
+    FastDiv page;
+};
+
+// The last index b in [0, n) with start[b] <= x, of a non-decreasing start[0] = 0 ... (the owner of element x: entries that
+// own nothing have the same start as the next one and are passed over).
+__device__ __forceinline__ int owner_of(const int* start, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(1024) page_plan_kernel(const PagePlanParams p)
+{
+    extern __shared__ int plan_smem[];
+    int* cached_s = plan_smem;                 // [B]
+    int* start_s = cached_s + p.B;             // [B]  first token
+    int* take_s = start_s + p.B;               // [B]  first page taken
+    int* give_s = take_s + p.B;                // [B]  first page given back
+    __shared__ int part[2][5][32];
+    const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
+    const int rank = blockIdx.x, everyone = gridDim.x * threads;
+    const unsigned full = 0xffffffffu;
+
+    const int count = *p.free_count;
+    int tokens = 0, taken = 0, given = 0;      // totals so far
+    long long tokens64 = 0;
+    bool bad = count < 0 || count > p.capacity;
+    for (int base = 0, turn = 0; base < p.B; base += threads, turn ^= 1) {
+        const int b = base + tid;
+        int tok = 0, take = 0, give = 0, c = 0;
+        if (b < p.B) {
+            c = p.cached[b];
+            const int a = p.added[b];
+            const long long most = (long long)p.width * p.page.d;
+            if (c < 0 || a < -1 || (long long)c + (a > 0 ? a : 0) > most) {
+                bad = true;
+            } else {
+                const int held = c ? (int)p.page.div((uint32_t)(c - 1)) + 1 : 0;
+                const int len = c + a;
+                if (a < 0) {
+                    give = held;
+                } else {
+                    tok = a;
+                    take = (len ? (int)p.page.div((uint32_t)(len - 1)) + 1 : 0) - held;
+                }
+            }
+        }
+        int s0 = tok, s1 = take, s2 = give;    // inclusive scans over the warp
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u0 = __shfl_up_sync(full, s0, o), u1 = __shfl_up_sync(full, s1, o), u2 = __shfl_up_sync(full, s2, o);
+            if (lane >= o) { s0 += u0; s1 += u1; s2 += u2; }
+        }
+        // Token sums may pass 2^31 where the step cannot fit: their halves are summed apart for the check.
+        const int lo = (int)__reduce_add_sync(full, (unsigned)tok & 0xffffu), hi = (int)__reduce_add_sync(full, (unsigned)tok >> 16);
+        if (lane == 31) { part[turn][0][warp] = s0; part[turn][1][warp] = s1; part[turn][2][warp] = s2; part[turn][3][warp] = lo; part[turn][4][warp] = hi; }
+        __syncthreads();
+        const int v0 = lane < warps ? part[turn][0][lane] : 0, v1 = lane < warps ? part[turn][1][lane] : 0, v2 = lane < warps ? part[turn][2][lane] : 0;
+        const unsigned vlo = lane < warps ? part[turn][3][lane] : 0, vhi = lane < warps ? part[turn][4][lane] : 0;
+        const bool before = lane < warp;
+        s0 += tokens + (int)__reduce_add_sync(full, before ? v0 : 0) - tok;
+        s1 += taken + (int)__reduce_add_sync(full, before ? v1 : 0) - take;
+        s2 += given + (int)__reduce_add_sync(full, before ? v2 : 0) - give;
+        tokens += (int)__reduce_add_sync(full, v0);
+        taken += (int)__reduce_add_sync(full, v1);
+        given += (int)__reduce_add_sync(full, v2);
+        tokens64 += (long long)__reduce_add_sync(full, vlo) + ((long long)__reduce_add_sync(full, vhi) << 16);
+        if (b < p.B) { cached_s[b] = c; start_s[b] = s0; take_s[b] = s1; give_s[b] = s2; }
+    }
+    bad = __syncthreads_or(bad);
+    const long long stack = (long long)count + given;
+    const int state = bad ? ATTN_PLAN_BAD_LENGTH
+                    : tokens64 > p.token_cap ? ATTN_PLAN_NO_ROOM
+                    : (taken > stack || stack - taken > p.capacity) ? ATTN_PLAN_NO_PAGES : ATTN_PLAN_FITS;
+    const bool fits = state == ATTN_PLAN_FITS;
+    // From here on `cached` and `free_count` may be overwritten by their outputs: all CTAs have read them.
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+    const int me = rank * threads + tid;
+    if (me == 0) {
+        *p.free_count_out = fits ? (int)(stack - taken) : count;
+        p.q_start[p.B] = fits ? tokens : 0;
+        p.info[0] = state;
+        p.info[1] = bad ? 0 : tokens64 > 2147483647 ? 2147483647 : (int)tokens64;
+        p.info[2] = bad ? 0 : taken;
+        p.info[3] = bad ? 0 : given;
+    }
+    auto page_returned = [&](int r) {
+        const int b = owner_of(give_s, p.B, r);
+        return p.table[(long long)b * p.table_stride + (r - give_s[b])];
+    };
+    auto page_taken = [&](int i) {
+        const int at = (int)(stack - 1) - i;
+        return at < count ? p.free_pages[at] : page_returned(at - count);
+    };
+    for (int b = me; b < p.B; b += everyone) {
+        const int next = b + 1 < p.B ? start_s[b + 1] : tokens, back = b + 1 < p.B ? give_s[b + 1] : given;
+        const int c = cached_s[b];
+        // A request that ends gives back at least a page, unless it holds none (and then its length is 0 already).
+        p.seq_len[b] = !fits ? c : back > give_s[b] ? 0 : c + (next - start_s[b]);
+        p.q_start[b] = fits ? start_s[b] : 0;
+    }
+    if (fits) {
+        for (int i = me; i < taken; i += everyone) {
+            const int b = owner_of(take_s, p.B, i), c = cached_s[b];
+            const int held = c ? (int)p.page.div((uint32_t)(c - 1)) + 1 : 0;
+            p.table[(long long)b * p.table_stride + held + (i - take_s[b])] = page_taken(i);
+        }
+        const int left = (int)(stack - taken) - count;   // returned pages that stay on the stack
+        for (int r = me; r < left; r += everyone) p.free_pages[count + r] = page_returned(r);
+    }
+    const int used = fits ? tokens : 0;
+    for (int t = me; t < p.token_cap; t += everyone) {
+        long long slot = -1;
+        int pos = 0, b = -1;
+        if (t < used) {
+            b = owner_of(start_s, p.B, t);
+            const int c = cached_s[b];
+            pos = c + (t - start_s[b]);
+            const int held = c ? (int)p.page.div((uint32_t)(c - 1)) + 1 : 0;
+            const int column = (int)p.page.div((uint32_t)pos);
+            const int page = column < held ? p.table[(long long)b * p.table_stride + column] : page_taken(take_s[b] + column - held);
+            slot = page < 0 ? -1 : (long long)page * p.page.d + (pos - column * (int)p.page.d);
+        }
+        p.slot[t] = slot;
+        if (p.position) p.position[t] = pos;
+        if (p.request) p.request[t] = b;
+    }
+}
+
+}  // namespace sawtooth

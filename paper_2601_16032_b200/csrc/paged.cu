@@ -1,0 +1,361 @@
+// C-ABI entry points around the paged key/value cache: argument checks and launches of the page plan and of the head norm
+// with rotation (forward with the append to the cache, and backward).
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "host.h"
+#include "page_plan.cuh"
+#include "qk_norm_rope.cuh"
+
+namespace {
+
+using namespace sawtooth;
+
+constexpr int kMaxPageSize = 65536;
+constexpr int kMaxHeads = 65536;
+constexpr int kRopeMaxCtas = 1024;     // of the backward pass; its workspace holds a partial sum of each
+
+enum RaisedBit { kRaisedPlan = 0, kRaisedDecode = 1 };
+
+// A rectangular region of memory: `outer` steps of `outer_stride`, each of `inner` steps of `inner_stride`, each of `bytes`.
+struct Region {
+    const void* p;
+    long long outer, outer_stride, inner, inner_stride, bytes;   // strides in bytes
+};
+bool spans_overlap(const Region& a, const Region& b) {
+    if (!a.p || !b.p || a.outer <= 0 || b.outer <= 0 || a.inner <= 0 || b.inner <= 0) return false;
+    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+    const uintptr_t a1 = a0 + (a.outer - 1) * a.outer_stride + (a.inner - 1) * a.inner_stride + a.bytes;
+    const uintptr_t b1 = b0 + (b.outer - 1) * b.outer_stride + (b.inner - 1) * b.inner_stride + b.bytes;
+    return a0 < b1 && b0 < a1;
+}
+// Two regions overlap.  Regions that interleave (queries and keys side by side in one array) do not: with equal outer strides
+// it is the offsets within one outer step that count.
+bool overlap(const Region& a, const Region& b) {
+    if (!spans_overlap(a, b)) return false;
+    if (a.outer_stride != b.outer_stride || a.outer_stride <= 0) return true;
+    const long long s = a.outer_stride, wa = (a.inner - 1) * a.inner_stride + a.bytes, wb = (b.inner - 1) * b.inner_stride + b.bytes;
+    if (wa > s || wb > s) return true;
+    const long long off = (long long)(((intptr_t)b.p - (intptr_t)a.p) % s + s) % s;   // of b's step behind the start of a's
+    return off < wa || off + wb > s;
+}
+bool same(const Region& a, const Region& b) {
+    return a.p == b.p && (a.outer <= 1 || a.outer_stride == b.outer_stride) && (a.inner <= 1 || a.inner_stride == b.inner_stride);
+}
+
+// n steps of `stride` elements stay far below the 64 bits of an address.
+bool fits_address(long long stride, long long n) { return stride <= (1ll << 55) / (n > 0 ? n : 1); }
+// All that lies between the first and the last row of one half of a cache.
+Region span_of(const attn_kv_cache& c, const void* p) {
+    return {p, 1, 0, 1, 0, 2 * ((c.num_pages - 1) * c.page_stride + (c.page_size - 1) * c.token_stride + (c.kv_heads - 1) * c.head_stride + c.d)};
+}
+
+int launch_status(cudaError_t e) {
+    if (e == cudaSuccess) return ATTN_OK;
+    cudaGetLastError();
+    return fail(ATTN_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
+// cudaLaunchKernelEx with a cluster of `cluster` CTAs (0: none) and, with `after`, the early launch behind the previous kernel
+// of the stream, which the kernel itself waits for.
+template <typename... Params, typename... Args>
+cudaError_t launch_ex(void (*kernel)(Params...), int grid_x, int grid_y, int threads, size_t smem, cudaStream_t stream, int cluster, bool after,
+                      Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid_x, (unsigned)grid_y);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (after) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+int check_head_shape(int H, int kv_heads, int d, int dtype) {
+    if (H <= 0 || kv_heads <= 0 || H > kMaxHeads || kv_heads > kMaxHeads)
+        return fail(ATTN_ERR_INVALID_ARG, "H and kv_heads must be in [1, %d] (got %d, %d)", kMaxHeads, H, kv_heads);
+    if (d != 64 && d != 128) return fail(ATTN_ERR_UNSUPPORTED, "head dimension %d is not supported (64 or 128)", d);
+    if (dtype != ATTN_F16 && dtype != ATTN_BF16) return fail(ATTN_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    return ATTN_OK;
+}
+
+// A cache descriptor with its strides filled in, checked.
+int check_cache(const attn_kv_cache* c, attn_kv_cache* out, bool written) {
+    if (!c) return fail(ATTN_ERR_INVALID_ARG, "cache is null");
+    *out = *c;
+    if (!c->k || !c->v) return fail(ATTN_ERR_INVALID_ARG, "the cache's k and v must be non-null");
+    int rc = check_head_shape(c->kv_heads, c->kv_heads, c->d, c->dtype);
+    if (rc) return rc;
+    if (c->page_size < 1 || c->page_size > kMaxPageSize) return fail(ATTN_ERR_INVALID_ARG, "page_size must be in [1, %d]", kMaxPageSize);
+    if (c->num_pages < 1 || c->num_pages > 2147483647ll) return fail(ATTN_ERR_INVALID_ARG, "num_pages must be in [1, 2^31-1]");
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15u) return fail(ATTN_ERR_ALIGNMENT, "the cache's k and v must be 16-byte aligned");
+    if (c->page_stride == 0 && c->token_stride == 0 && c->head_stride == 0) {
+        if (c->layout != ATTN_LAYOUT_BHND && c->layout != ATTN_LAYOUT_BNHD) return fail(ATTN_ERR_INVALID_ARG, "unknown layout %d", c->layout);
+        out->page_stride = (long long)c->page_size * c->kv_heads * c->d;
+        out->token_stride = c->layout == ATTN_LAYOUT_BNHD ? (long long)c->kv_heads * c->d : c->d;
+        out->head_stride = c->layout == ATTN_LAYOUT_BNHD ? c->d : (long long)c->page_size * c->d;
+    }
+    if (c->k == c->v) return fail(ATTN_ERR_INVALID_ARG, "the cache's k and v must not be the same array");
+    if ((out->page_stride | out->token_stride | out->head_stride) & 7)
+        return fail(ATTN_ERR_INVALID_ARG, "the cache's strides must be multiples of 8 elements");
+    if (out->page_stride < 0 || out->token_stride < 0 || out->head_stride < 0) return fail(ATTN_ERR_INVALID_ARG, "the cache's strides must not be negative");
+    if (!fits_address(out->page_stride, c->num_pages) || !fits_address(out->token_stride, c->page_size) || !fits_address(out->head_stride, c->kv_heads))
+        return fail(ATTN_ERR_INVALID_ARG, "the cache's strides reach too far");
+    if (written) {
+        // Rows that share memory could not all be written: from the shortest stride up, a step clears what lies below it.
+        struct { long long stride, n; } dim[3] = {{out->page_stride, c->num_pages}, {out->token_stride, c->page_size}, {out->head_stride, c->kv_heads}};
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2 - i; ++j)
+                if (dim[j].stride > dim[j + 1].stride) { auto t = dim[j]; dim[j] = dim[j + 1]; dim[j + 1] = t; }
+        long long need = c->d;
+        for (auto& x : dim) {
+            if (x.n <= 1) continue;
+            if (x.stride < need) return fail(ATTN_ERR_INVALID_ARG, "the cache's strides make its rows overlap");
+            need = x.stride * (x.n - 1) + need;
+        }
+    }
+    return ATTN_OK;
+}
+
+CacheView view_of(const attn_kv_cache& c) {
+    CacheView v;
+    v.k = static_cast<const uint16_t*>(c.k);
+    v.v = static_cast<const uint16_t*>(c.v);
+    v.page_stride = c.page_stride;
+    v.token_stride = c.token_stride;
+    v.head_stride = c.head_stride;
+    v.num_pages = c.num_pages;
+    v.page = FastDiv((uint32_t)c.page_size);
+    return v;
+}
+
+// [outer, inner, d] 16-bit rows at the given strides (elements; both 0 = contiguous), checked.
+int rows_of(const char* name, const void* p, long long outer_stride, long long inner_stride, long long outer, long long inner, int d, bool written,
+            Region* out) {
+    if (!p) return fail(ATTN_ERR_INVALID_ARG, "%s must be non-null", name);
+    if ((uintptr_t)p & 15u) return fail(ATTN_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
+    if (outer_stride == 0 && inner_stride == 0) { outer_stride = inner * d; inner_stride = d; }
+    if ((outer_stride | inner_stride) & 7) return fail(ATTN_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements", name);
+    if (outer_stride < 0 || inner_stride < 0 || !fits_address(outer_stride, outer) || !fits_address(inner_stride, inner))
+        return fail(ATTN_ERR_INVALID_ARG, "%s: strides are negative or reach too far", name);
+    if (written) {
+        const bool outer_first = outer_stride < inner_stride;
+        const long long n0 = outer_first ? outer : inner, s0 = outer_first ? outer_stride : inner_stride;
+        const long long n1 = outer_first ? inner : outer, s1 = outer_first ? inner_stride : outer_stride;
+        if ((n0 > 1 && s0 < d) || (n1 > 1 && s1 < (n0 > 1 ? (n0 - 1) * s0 : 0) + d)) return fail(ATTN_ERR_INVALID_ARG, "%s: strides make its rows overlap", name);
+    }
+    *out = {p, outer, outer_stride * 2, inner, inner_stride * 2, (long long)d * 2};
+    return ATTN_OK;
+}
+RopeTensor in_of(const Region& r) { return {static_cast<const uint16_t*>(r.p), r.outer_stride / 2, r.inner_stride / 2}; }
+RopeOut out_of(const Region& r) { return {static_cast<uint16_t*>(const_cast<void*>(r.p)), r.outer_stride / 2, r.inner_stride / 2}; }
+
+int check_rope(int T, int H, int kv_heads, int d, int dtype, const void* q_weight, const void* k_weight, float eps, const int* position,
+               const double* inv_freq, int rot_dim, int rot_style, const attn_rope_opts& z) {
+    if (T < 0 || T > (1 << 30)) return fail(ATTN_ERR_INVALID_ARG, "T must be in [0, 2^30]");
+    int rc = check_head_shape(H, kv_heads, d, dtype);
+    if (rc) return rc;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(ATTN_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (rot_dim < 0 || rot_dim > d || rot_dim % 16) return fail(ATTN_ERR_INVALID_ARG, "rot_dim must be a multiple of 16 in [0, d]");
+    if (rot_style != ATTN_ROPE_HALVES && rot_style != ATTN_ROPE_ADJACENT) return fail(ATTN_ERR_INVALID_ARG, "unknown rot_style %d", rot_style);
+    if (rot_dim && (!position || !inv_freq)) return fail(ATTN_ERR_INVALID_ARG, "a rotation needs position and inv_freq");
+    if ((uintptr_t)position & 3u || (uintptr_t)inv_freq & 7u) return fail(ATTN_ERR_ALIGNMENT, "position and inv_freq must be aligned to their elements");
+    if (((uintptr_t)q_weight | (uintptr_t)k_weight) & 15u) return fail(ATTN_ERR_ALIGNMENT, "the weights must be 16-byte aligned");
+    if (z.weight_f32 != 0 && z.weight_f32 != 1) return fail(ATTN_ERR_INVALID_ARG, "weight_f32 must be 0 or 1");
+    if (z.check_mode != 0 && z.check_mode != 1) return fail(ATTN_ERR_INVALID_ARG, "check_mode must be 0 or 1");
+    return ATTN_OK;
+}
+
+void fill_rope(RopeParams* p, int T, int H, int kv_heads, const void* q_weight, const void* k_weight, float eps, const int* position,
+               const double* inv_freq, int rot_dim, const attn_rope_opts& z, const DeviceState& ds) {
+    p->q_weight = q_weight;
+    p->k_weight = k_weight;
+    p->position = position;
+    p->inv_freq = inv_freq;
+    p->status = ds.status;
+    p->eps = eps;
+    p->T = T;
+    p->H = H;
+    p->kv_heads = kv_heads;
+    p->rot = rot_dim;
+    p->weight_f32 = z.weight_f32;
+}
+
+using RopeKernel = void (*)(const RopeParams);
+template <int kD, int kBf16>
+RopeKernel rope_kernel_of(int style, bool backward) {
+    if (backward) return style ? qk_norm_rope_bwd_kernel<kD, kBf16, 1> : qk_norm_rope_bwd_kernel<kD, kBf16, 0>;
+    return style ? qk_norm_rope_kernel<kD, kBf16, 1> : qk_norm_rope_kernel<kD, kBf16, 0>;
+}
+RopeKernel rope_kernel(int d, int dtype, int style, bool backward) {
+    if (d == 128) return dtype == ATTN_BF16 ? rope_kernel_of<128, 1>(style, backward) : rope_kernel_of<128, 0>(style, backward);
+    return dtype == ATTN_BF16 ? rope_kernel_of<64, 1>(style, backward) : rope_kernel_of<64, 0>(style, backward);
+}
+
+}  // namespace
+
+extern "C" {
+
+int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* added, int B, int* seq_len, int* q_start, long long* slot,
+                   int* position, int* request, int token_cap, int* info, void* stream) {
+    if (!pool || !cached || !added || !seq_len || !q_start || !info || !pool->block_table || !pool->free_pages || !pool->free_count ||
+        !pool->free_count_out || (!slot && token_cap > 0))
+        return fail(ATTN_ERR_INVALID_ARG, "pool, cached, added, seq_len, q_start, slot, info and the pool's arrays must be non-null");
+    if (B < 1 || B > kPlanMaxRequests) return fail(ATTN_ERR_INVALID_ARG, "B must be in [1, %d]", kPlanMaxRequests);
+    if (token_cap < 0) return fail(ATTN_ERR_INVALID_ARG, "token_cap must not be negative");
+    if (pool->page_size < 1 || pool->page_size > kMaxPageSize) return fail(ATTN_ERR_INVALID_ARG, "page_size must be in [1, %d]", kMaxPageSize);
+    if (pool->width < 1 || pool->capacity < 0) return fail(ATTN_ERR_INVALID_ARG, "width must be positive and capacity not negative");
+    if ((long long)pool->width * pool->page_size > 2147483647ll || (long long)pool->width * B > 2147483647ll)
+        return fail(ATTN_ERR_INVALID_ARG, "width * page_size and width * B must be below 2^31");
+    if (pool->table_stride < pool->width) return fail(ATTN_ERR_INVALID_ARG, "table_stride must be at least width");
+    if (((uintptr_t)cached | (uintptr_t)added | (uintptr_t)seq_len | (uintptr_t)q_start | (uintptr_t)position | (uintptr_t)request | (uintptr_t)info |
+         (uintptr_t)pool->block_table | (uintptr_t)pool->free_pages | (uintptr_t)pool->free_count | (uintptr_t)pool->free_count_out) & 3u ||
+        (uintptr_t)slot & 7u)
+        return fail(ATTN_ERR_ALIGNMENT, "arrays must be aligned to their elements");
+    auto line = [](const void* a, long long n, long long size) { return Region{a, 1, 0, 1, 0, n * size}; };
+    const Region in[] = {line(cached, B, 4), line(added, B, 4), line(pool->free_count, 1, 4)};
+    const Region out[] = {line(seq_len, B, 4), line(pool->free_count_out, 1, 4), line(q_start, B + 1, 4), line(slot, token_cap, 8), line(position, token_cap, 4),
+                          line(request, token_cap, 4), line(info, 4, 4), line(pool->free_pages, pool->capacity, 4),
+                          line(pool->block_table, (B - 1) * pool->table_stride + pool->width, 4)};
+    constexpr int kOut = sizeof(out) / sizeof(out[0]);
+    for (int i = 0; i < kOut; ++i) {
+        for (int j = 0; j < 3; ++j) {
+            const bool allowed = (i == 0 && j == 0 && seq_len == cached) || (i == 1 && j == 2 && pool->free_count_out == pool->free_count);
+            if (out[i].bytes > 0 && !allowed && spans_overlap(out[i], in[j])) return fail(ATTN_ERR_INVALID_ARG, "the plan's arrays overlap");
+        }
+        for (int j = i + 1; j < kOut; ++j)
+            if (out[i].bytes > 0 && out[j].bytes > 0 && spans_overlap(out[i], out[j])) return fail(ATTN_ERR_INVALID_ARG, "the plan's arrays overlap");
+    }
+    DeviceState ds;
+    int dev = 0;
+    int rc = current_device(&ds, &dev);
+    if (rc) return rc;
+    PagePlanParams p;
+    p.cached = cached; p.added = added; p.table = pool->block_table; p.table_stride = pool->table_stride;
+    p.free_pages = pool->free_pages; p.free_count = pool->free_count; p.free_count_out = pool->free_count_out;
+    p.seq_len = seq_len; p.q_start = q_start; p.slot = slot; p.position = position; p.request = request; p.info = info;
+    p.B = B; p.width = pool->width; p.capacity = pool->capacity; p.token_cap = token_cap;
+    p.page = FastDiv((uint32_t)pool->page_size);
+    const size_t smem = (size_t)B * 4 * sizeof(int);
+    if (smem > 40 * 1024 && (rc = raise_smem(dev, ds, (const void*)page_plan_kernel, kRaisedPlan, kPlanMaxRequests * 16))) return rc;
+    const long long items = (long long)token_cap + B;
+    const int threads = items <= 512 ? 256 : 1024;
+    const int cluster = items <= 4096 ? 1 : 8;
+    return launch_status(launch_ex(page_plan_kernel, cluster, 1, threads, smem, static_cast<cudaStream_t>(stream), cluster, false, p));
+}
+
+int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out, int T, int H, int kv_heads, int d, int dtype,
+                      const void* q_weight, const void* k_weight, float eps, const int* position, const double* inv_freq, int rot_dim,
+                      int rot_style, void* stream, const attn_rope_opts* opts) {
+    attn_rope_opts z;
+    memset(&z, 0, sizeof(z));
+    if (opts) z = *opts;
+    int rc = check_rope(T, H, kv_heads, d, dtype, q_weight, k_weight, eps, position, inv_freq, rot_dim, rot_style, z);
+    if (rc) return rc;
+    if ((z.cache != nullptr) != (z.slot != nullptr) || (z.cache != nullptr) != (v != nullptr))
+        return fail(ATTN_ERR_INVALID_ARG, "cache, slot and v go together: all of them or none");
+    if (!z.cache && !k_out) return fail(ATTN_ERR_INVALID_ARG, "k_out may be null only when there is a cache");
+    RopeParams p = {};
+    Region rq, rk, rv = {}, rqo, rko = {};
+    if ((rc = rows_of("q", q, z.q_token, z.q_head, T, H, d, false, &rq)) || (rc = rows_of("k", k, z.k_token, z.k_head, T, kv_heads, d, false, &rk)) ||
+        (rc = rows_of("q_out", q_out, z.q_out_token, z.q_out_head, T, H, d, true, &rqo)))
+        return rc;
+    if (k_out && (rc = rows_of("k_out", k_out, z.k_out_token, z.k_out_head, T, kv_heads, d, true, &rko))) return rc;
+    p.rows = FastDiv((uint32_t)(H + kv_heads));
+    if (z.cache) {
+        if ((rc = rows_of("v", v, z.v_token, z.v_head, T, kv_heads, d, false, &rv))) return rc;
+        attn_kv_cache c;
+        if ((rc = check_cache(z.cache, &c, true))) return rc;
+        if (c.kv_heads != kv_heads || c.d != d || c.dtype != dtype) return fail(ATTN_ERR_INVALID_ARG, "the cache's heads, head dimension or type differ from the call's");
+        if ((uintptr_t)z.slot & 7u) return fail(ATTN_ERR_ALIGNMENT, "slot must be 8-byte aligned");
+        for (const Region& half : {span_of(c, c.k), span_of(c, c.v)})
+            if (spans_overlap(half, rq) || spans_overlap(half, rk) || spans_overlap(half, rv) || spans_overlap(half, rqo) || spans_overlap(half, rko))
+                return fail(ATTN_ERR_INVALID_ARG, "the cache must not overlap the call's other arrays");
+        p.cache = view_of(c);
+        p.slot = z.slot;
+        p.rows = FastDiv((uint32_t)(H + 2 * kv_heads));
+    }
+    if ((overlap(rqo, rq) && !same(rqo, rq)) || overlap(rqo, rk) || overlap(rqo, rv) || overlap(rqo, rko) || (overlap(rko, rk) && !same(rko, rk)) ||
+        overlap(rko, rq) || overlap(rko, rv))
+        return fail(ATTN_ERR_INVALID_ARG, "q_out and k_out may be q and k themselves, but overlap nothing otherwise");
+    DeviceState ds;
+    if ((rc = current_device(&ds, nullptr))) return rc;
+    if (T == 0) return ATTN_OK;
+    fill_rope(&p, T, H, kv_heads, q_weight, k_weight, eps, position, inv_freq, rot_dim, z, ds);
+    p.q = in_of(rq); p.k = in_of(rk); p.q_out = out_of(rqo);
+    if (k_out) p.k_out = out_of(rko);
+    if (z.cache) p.v = in_of(rv);
+    p.tokens_per_cta = T <= 4 * ds.sm_count ? 1 : 2;
+    const int grid = (T + p.tokens_per_cta - 1) / p.tokens_per_cta;
+    rope_kernel(d, dtype, rot_style, false)<<<grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+    if ((rc = launch_status(cudaGetLastError()))) return rc;
+    return z.check_mode ? read_status(nullptr) : ATTN_OK;
+}
+
+size_t attn_rope_bwd_workspace_bytes(int d) { return d > 0 ? (size_t)kRopeMaxCtas * 2 * sizeof(float) * (size_t)d : 0; }
+
+int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, void* dq, void* dk, float* dq_weight,
+                          float* dk_weight, int T, int H, int kv_heads, int d, int dtype, const void* q_weight, const void* k_weight,
+                          float eps, const int* position, const double* inv_freq, int rot_dim, int rot_style, void* workspace,
+                          size_t workspace_bytes, void* stream, const attn_rope_opts* opts) {
+    attn_rope_opts z;
+    memset(&z, 0, sizeof(z));
+    if (opts) z = *opts;
+    int rc = check_rope(T, H, kv_heads, d, dtype, q_weight, k_weight, eps, position, inv_freq, rot_dim, rot_style, z);
+    if (rc) return rc;
+    if (z.cache || z.slot) return fail(ATTN_ERR_INVALID_ARG, "the backward pass has no cache");
+    if ((q_weight != nullptr) != (dq_weight != nullptr) || (k_weight != nullptr) != (dk_weight != nullptr))
+        return fail(ATTN_ERR_INVALID_ARG, "dq_weight and dk_weight must be null exactly where the weights are");
+    if (((uintptr_t)dq_weight | (uintptr_t)dk_weight) & 3u) return fail(ATTN_ERR_ALIGNMENT, "dq_weight and dk_weight must be 4-byte aligned");
+    if (!workspace || workspace_bytes < attn_rope_bwd_workspace_bytes(d))
+        return fail(ATTN_ERR_INVALID_ARG, "the workspace needs %zu bytes", attn_rope_bwd_workspace_bytes(d));
+    if ((uintptr_t)workspace & 15u) return fail(ATTN_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
+    RopeParams p = {};
+    Region rq, rk, rgq, rgk, rdq, rdk;
+    if ((rc = rows_of("q", q, z.q_token, z.q_head, T, H, d, false, &rq)) || (rc = rows_of("k", k, z.k_token, z.k_head, T, kv_heads, d, false, &rk)) ||
+        (rc = rows_of("dq_out", dq_out, z.q_out_token, z.q_out_head, T, H, d, false, &rgq)) ||
+        (rc = rows_of("dk_out", dk_out, z.k_out_token, z.k_out_head, T, kv_heads, d, false, &rgk)) ||
+        (rc = rows_of("dq", dq, z.dq_token, z.dq_head, T, H, d, true, &rdq)) || (rc = rows_of("dk", dk, z.dk_token, z.dk_head, T, kv_heads, d, true, &rdk)))
+        return rc;
+    const Region ws = {workspace, 1, 0, 1, 0, (long long)attn_rope_bwd_workspace_bytes(d)};
+    if (overlap(rdq, rq) || overlap(rdq, rk) || overlap(rdq, rgk) || (overlap(rdq, rgq) && !same(rdq, rgq)) || overlap(rdq, rdk) || overlap(rdk, rq) ||
+        overlap(rdk, rk) || overlap(rdk, rgq) || (overlap(rdk, rgk) && !same(rdk, rgk)) || overlap(ws, rq) || overlap(ws, rk) || overlap(ws, rgq) ||
+        overlap(ws, rgk) || overlap(ws, rdq) || overlap(ws, rdk))
+        return fail(ATTN_ERR_INVALID_ARG, "dq and dk may be dq_out and dk_out themselves, but overlap nothing otherwise");
+    DeviceState ds;
+    if ((rc = current_device(&ds, nullptr))) return rc;
+    fill_rope(&p, T, H, kv_heads, q_weight, k_weight, eps, position, inv_freq, rot_dim, z, ds);
+    p.q = in_of(rq); p.k = in_of(rk); p.dq_out = in_of(rgq); p.dk_out = in_of(rgk); p.q_out = out_of(rdq); p.k_out = out_of(rdk);
+    p.rows = FastDiv((uint32_t)(H + kv_heads));
+    p.partial = static_cast<float*>(workspace);
+    p.tokens_per_cta = T <= 4 * ds.sm_count ? 1 : 2;
+    const int chunks = (T + p.tokens_per_cta - 1) / p.tokens_per_cta;
+    int grid = 4 * ds.sm_count < kRopeMaxCtas ? 4 * ds.sm_count : kRopeMaxCtas;
+    if (grid > chunks) grid = chunks > 0 ? chunks : 1;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    rope_kernel(d, dtype, rot_style, true)<<<grid, kRopeThreads, 0, st>>>(p);
+    if ((rc = launch_status(cudaGetLastError()))) return rc;
+    if (dq_weight || dk_weight) {
+        rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 32, 1, 1024, 0, st, 0, true, (const float*)p.partial, grid, d, dq_weight, dk_weight));
+        if (rc) return rc;
+    }
+    return z.check_mode ? read_status(nullptr) : ATTN_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,61 @@
+// Shared by the kernels around the paged cache: division by a run-time constant, the cache as kernels see it, 16-bit pairs.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ptx.cuh"
+
+namespace sawtooth {
+
+// n / d for 0 <= n < 2^31 by one multiplication: with l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1 the quotient
+// is (mulhi(n, m) + n) >> l (Granlund and Montgomery, "Division by Invariant Integers using Multiplication", 1994).
+struct FastDiv {
+    uint32_t d = 1, m = 1, l = 0;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t divisor) : d(divisor) {
+        l = 0;
+        while ((1ull << l) < divisor) ++l;
+        m = (uint32_t)(((1ull << 32) * ((1ull << l) - divisor)) / divisor + 1);
+    }
+    __host__ __device__ uint32_t div(uint32_t n) const {
+#ifdef __CUDA_ARCH__
+        return (__umulhi(n, m) + n) >> l;
+#else
+        return ((uint32_t)(((uint64_t)n * m) >> 32) + n) >> l;
+#endif
+    }
+};
+
+struct CacheView {
+    const uint16_t* k;
+    const uint16_t* v;
+    long long page_stride, token_stride, head_stride;
+    long long num_pages;
+    FastDiv page;   // page.d = tokens per page
+};
+
+__device__ __forceinline__ void note_index(int* status, int code) { atomicCAS(status, 0, code); }
+
+template <int kBf16>
+__device__ __forceinline__ void unpack2(uint32_t u, float& lo, float& hi) {
+    if (kBf16) {
+        lo = __uint_as_float(u << 16);
+        hi = __uint_as_float(u & 0xffff0000u);
+    } else {
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(u));
+    }
+}
+
+template <int kBf16>
+__device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
+    unpack2<kBf16>(u.x, x[0], x[1]);
+    unpack2<kBf16>(u.y, x[2], x[3]);
+    unpack2<kBf16>(u.z, x[4], x[5]);
+    unpack2<kBf16>(u.w, x[6], x[7]);
+}
+template <int kBf16>
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+    return make_uint4(ptx::pack2<kBf16>(x[0], x[1]), ptx::pack2<kBf16>(x[2], x[3]), ptx::pack2<kBf16>(x[4], x[5]), ptx::pack2<kBf16>(x[6], x[7]));
+}
+
+}  // namespace sawtooth
