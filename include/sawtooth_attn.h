@@ -245,8 +245,9 @@ int attn_dynamic_claim_trace(int B, int H, int N, int d, int causal, int scan_or
 
 /* ------------------------------------------------------------------------------------------------------------------
  * Around the attention kernel in a server (outside the paper): keys and values kept in pages, the tables that say which
- * page holds what, and the step that puts new keys and values there.
- * A step is: attn_page_plan (once for all layers), then per layer attn_qk_norm_rope on the projections.  All of it can be captured into a CUDA graph: lengths,
+ * page holds what, the step that puts new keys and values there, and attention of one new token per request over them.
+ * A step is: attn_page_plan (once for all layers), then per layer attn_qk_norm_rope on the projections, and attn_fwd
+ * (prompts) or attn_decode_paged (one new token per request).  All of it can be captured into a CUDA graph: lengths,
  * tables and the pool of free pages live on the device.
  *
  * A device's first call of an entry point looks symbols up and raises limits (make it outside any stream capture);
@@ -363,6 +364,58 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
                           float* dk_weight, int T, int H, int kv_heads, int d, int dtype, const void* q_weight, const void* k_weight,
                           float eps, const int* position, const double* inv_freq, int rot_dim, int rot_style, void* workspace,
                           size_t workspace_bytes, void* stream, const attn_rope_opts* opts);
+
+/*
+ * Attention of one new token per request over the cache: for request b and query head h, over its first seq_len[b] tokens,
+ *     o[b,h,:] = sum_j softmax_j( scale * q[b,h,:] . K[j,:] ) * V[j,:],
+ * K and V those of head h / (H / kv_heads), token j in page block_table[b * table_stride + j / page_size] at j % page_size.
+ * (The new token's own key and value are in the cache already, see attn_qk_norm_rope, and seq_len counts it.)  seq_len 0: o = 0,
+ * lse = -infinity.  Table entries behind a request's last page are not read; cache contents behind its last token do not matter,
+ * whatever they are.  A length below 0 or above max_pages * page_size is cut to that range, a page number outside [0, num_pages) reads
+ * as zeros; both are noted in the status word and that request's o is then of no use.
+ *
+ * The work is cut over the length: the 64-token tiles of all requests and K/V heads, in that order, are dealt out to the CTAs in equal
+ * contiguous shares whatever the lengths (attn_decode_trace replays it), and requests cut by a share's border are joined by
+ * their running maxima and sums.  For fixed arguments bitwise reproducible.  The products take their 16-bit operands as they are;
+ * probabilities enter the second product as the sum of two 16-bit numbers; sums are fp32; o is rounded once.
+ *
+ * q, o: [B, H, d], strides in opts, d elements contiguous, 16-byte aligned, strides multiples of 8.  o must not overlap q, the
+ * cache or the workspace.  workspace: as many bytes as attn_decode_query_plan says, 16-byte aligned, contents of no matter; calls that share one must
+ * not overlap on the GPU (graphs included).
+ */
+typedef struct {
+    long long q_request, q_head, o_request, o_head;   /* strides in elements; each pair both 0 = contiguous [B, H, d] */
+    float* lse;       /* optional DEVICE output [B, H] fp32: ln sum_j exp(scale * q . K[j]) */
+    int max_ctas;     /* cap on the grid; 0: what fits on the GPU at a time */
+    int check_mode;   /* as in attn_fwd_opts */
+    int reserved[2];
+} attn_decode_opts;
+
+typedef struct {
+    int grid, threads, smem_bytes;
+    int tile_tokens;         /* tokens of a tile */
+    int head_blocks;         /* blocks of up to 16 query heads that read one K/V head */
+    int min_tiles;           /* a CTA's share is at least this many tiles (but for rounding) */
+    size_t workspace_bytes;
+} attn_decode_plan;
+
+/* One piece of work of a CTA, in the order it handles them (host-side replay of the device's arithmetic). */
+typedef struct {
+    int cta, request, kv_head, head_block;
+    int tile_begin, tile_end;   /* of the request's tiles */
+    int n_tiles;                /* tiles the request has */
+    int part;                   /* workspace entry the piece's partial result goes to; -1: complete, written to o */
+    int first_cta, last_cta;    /* CTAs that share the request's tiles of this head */
+} attn_decode_trace_entry;
+
+/* What a call will launch.  sm_count <= 0 asks the current device. */
+int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count, attn_decode_plan* out);
+int attn_decode_trace(const int* seq_len_host, int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count,
+                      attn_decode_trace_entry* buf, size_t cap, size_t* n);
+
+int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* block_table, long long table_stride, int max_pages,
+                      const int* seq_len, void* o, int B, int H, float scale, void* workspace, size_t workspace_bytes, void* stream,
+                      const attn_decode_opts* opts);
 
 /*
  * Waits for the current device and reads, then clears, its kernel status word: 0, or a code naming

@@ -81,6 +81,22 @@ class RopeOpts(ctypes.Structure):
     ]
 
 
+class DecodeOpts(ctypes.Structure):
+    """attn_decode_opts: strides in elements (a pair of zeros: contiguous); 0 otherwise means 'library default'."""
+    _fields_ = [(name, ctypes.c_longlong) for name in ("q_request", "q_head", "o_request", "o_head")] + [
+        ("lse", ctypes.c_void_p), ("max_ctas", ctypes.c_int), ("check_mode", ctypes.c_int), ("reserved", ctypes.c_int * 2)]
+
+
+class DecodePlan(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("grid", "threads", "smem_bytes", "tile_tokens", "head_blocks", "min_tiles")] + [
+        ("workspace_bytes", ctypes.c_size_t)]
+
+
+class DecodeTraceEntry(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("cta", "request", "kv_head", "head_block", "tile_begin", "tile_end", "n_tiles", "part", "first_cta",
+                                                  "last_cta")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -119,7 +135,12 @@ def load_library():
     lib.attn_rope_bwd_workspace_bytes.argtypes = [ci]
     lib.attn_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [ci] * 5 + [vp, vp, cf, vp, vp, ci, ci, vp, ctypes.c_size_t, vp, ctypes.POINTER(RopeOpts)]
-    for name in ("attn_page_plan", "attn_qk_norm_rope", "attn_qk_norm_rope_bwd"):
+    lib.attn_decode_query_plan.argtypes = [ci, ci, ci, ci, ctypes.POINTER(DecodeOpts), ci, ctypes.POINTER(DecodePlan)]
+    lib.attn_decode_trace.argtypes = [ctypes.POINTER(ci), ci, ci, ci, ci, ctypes.POINTER(DecodeOpts), ci, ctypes.POINTER(DecodeTraceEntry), ctypes.c_size_t,
+                                      ctypes.POINTER(ctypes.c_size_t)]
+    lib.attn_decode_paged.argtypes = [vp, ctypes.POINTER(KVCache), vp, ctypes.c_longlong, ci, vp, vp, ci, ci, cf, vp, ctypes.c_size_t, vp,
+                                      ctypes.POINTER(DecodeOpts)]
+    for name in ("attn_page_plan", "attn_qk_norm_rope", "attn_qk_norm_rope_bwd", "attn_decode_query_plan", "attn_decode_trace", "attn_decode_paged"):
         getattr(lib, name).restype = ci
     for name in ("attn_fwd", "attn_fwd_ex", "attn_fwd_host", "attn_query_plan", "attn_schedule_trace", "attn_device_status"):
         getattr(lib, name).restype = ci
@@ -244,6 +265,28 @@ def attn_qk_norm_rope_bwd(dq_out: int, dk_out: int, q: int, k: int, dq: int, dk:
                           workspace: int, workspace_bytes: int, stream: int = 0, opts: Optional[RopeOpts] = None) -> None:
     _check(load_library().attn_qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, dq_weight, dk_weight, T, H, kv_heads, d, dtype, q_weight, k_weight, eps,
                                                 position, inv_freq, rot_dim, rot_style, workspace, workspace_bytes, stream, _opts_ptr(opts)))
+
+
+def attn_decode_query_plan(B: int, H: int, kv_heads: int, d: int, opts: Optional[DecodeOpts] = None, sm_count: int = 0) -> DecodePlan:
+    plan = DecodePlan()
+    _check(load_library().attn_decode_query_plan(B, H, kv_heads, d, _opts_ptr(opts), sm_count, ctypes.byref(plan)))
+    return plan
+
+
+def attn_decode_trace(seq_len, H: int, kv_heads: int, d: int, opts: Optional[DecodeOpts] = None, sm_count: int = 0) -> list:
+    """Host-only replay of how a decode over requests of these lengths is dealt out to the CTAs."""
+    lib, B = load_library(), len(seq_len)
+    lens, n = (ctypes.c_int * max(1, B))(*seq_len), ctypes.c_size_t(0)
+    _check(lib.attn_decode_trace(lens, B, H, kv_heads, d, _opts_ptr(opts), sm_count, None, 0, ctypes.byref(n)))
+    buf = (DecodeTraceEntry * max(1, n.value))()
+    _check(lib.attn_decode_trace(lens, B, H, kv_heads, d, _opts_ptr(opts), sm_count, buf, n.value, ctypes.byref(n)))
+    return list(buf)[:n.value]
+
+
+def attn_decode_paged(q: int, cache: KVCache, block_table: int, table_stride: int, max_pages: int, seq_len: int, o: int, B: int, H: int, scale: float,
+                      workspace: int, workspace_bytes: int, stream: int = 0, opts: Optional[DecodeOpts] = None) -> None:
+    _check(load_library().attn_decode_paged(q, ctypes.byref(cache), block_table, table_stride, max_pages, seq_len, o, B, H, scale, workspace,
+                                            workspace_bytes, stream, _opts_ptr(opts)))
 
 
 def attn_device_status() -> int:

@@ -1,5 +1,5 @@
-// C-ABI entry points around the paged key/value cache: argument checks and launches of the page plan and of the head norm
-// with rotation (forward with the append to the cache, and backward).
+// C-ABI entry points around the paged key/value cache: argument checks and launches of the page plan, of the head norm with
+// rotation (forward with the append to the cache, and backward) and of the paged decode.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -7,6 +7,7 @@
 #include <cstring>
 
 #include "host.h"
+#include "decode_sm100.cuh"
 #include "page_plan.cuh"
 #include "qk_norm_rope.cuh"
 
@@ -208,6 +209,37 @@ RopeKernel rope_kernel(int d, int dtype, int style, bool backward) {
     return dtype == ATTN_BF16 ? rope_kernel_of<64, 1>(style, backward) : rope_kernel_of<64, 0>(style, backward);
 }
 
+using DecodeKernel = void (*)(const DecodeParams);
+template <int kD, int kBf16>
+int launch_decode(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
+    constexpr int kSmem = DecodeGeometry<kD>::kSmem;
+    DecodeKernel kernel = decode_paged_kernel<kD, kBf16>;
+    int rc = raise_smem(dev, ds, (const void*)kernel, kRaisedDecode + (kD == 128) * 2 + kBf16, kSmem);
+    if (rc) return rc;
+    if ((rc = launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, 0, false, p)))) return rc;
+    const int rows = p.group < kDecodeRows ? p.group : kDecodeRows;
+    return launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, rows, kJoinThreads, 0, st, 0, true, p));
+}
+
+size_t decode_workspace(int grid, int d) {
+    return (size_t)grid * (sizeof(int4) + 2 * kDecodeRows * (sizeof(float2) + sizeof(float) * (size_t)d));
+}
+
+int check_decode_shape(int B, int H, int kv_heads, int d, const attn_decode_opts& z) {
+    if (B <= 0) return fail(ATTN_ERR_INVALID_ARG, "B must be positive");
+    int rc = check_head_shape(H, kv_heads, d, ATTN_F16);
+    if (rc) return rc;
+    if (H % kv_heads) return fail(ATTN_ERR_INVALID_ARG, "kv_heads (%d) must divide the number of query heads (%d)", kv_heads, H);
+    if ((long long)B * H > 2147483647ll) return fail(ATTN_ERR_INVALID_ARG, "B*H exceeds 2^31-1");
+    if (z.max_ctas < 0) return fail(ATTN_ERR_INVALID_ARG, "max_ctas must be >= 0");
+    if (z.check_mode != 0 && z.check_mode != 1) return fail(ATTN_ERR_INVALID_ARG, "check_mode must be 0 or 1");
+    return ATTN_OK;
+}
+int decode_grid(int sm_count, const attn_decode_opts& z) {
+    const int most = 2 * sm_count;   // two CTAs of 96 KiB an SM
+    return z.max_ctas > 0 && z.max_ctas < most ? z.max_ctas : most;
+}
+
 }  // namespace
 
 extern "C" {
@@ -355,6 +387,139 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
         rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 32, 1, 1024, 0, st, 0, true, (const float*)p.partial, grid, d, dq_weight, dk_weight));
         if (rc) return rc;
     }
+    return z.check_mode ? read_status(nullptr) : ATTN_OK;
+}
+
+int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count, attn_decode_plan* out) {
+    if (!out) return fail(ATTN_ERR_INVALID_ARG, "out is null");
+    attn_decode_opts z;
+    memset(&z, 0, sizeof(z));
+    if (opts) z = *opts;
+    int rc = check_decode_shape(B, H, kv_heads, d, z);
+    if (rc) return rc;
+    if (sm_count <= 0) {
+        DeviceState ds;
+        if ((rc = current_device(&ds, nullptr))) return rc;
+        sm_count = ds.sm_count;
+    }
+    out->grid = decode_grid(sm_count, z);
+    out->threads = kDecodeThreads;
+    out->smem_bytes = d == 128 ? DecodeGeometry<128>::kSmem : DecodeGeometry<64>::kSmem;
+    out->tile_tokens = kDecodeTile;
+    out->head_blocks = (H / kv_heads + kDecodeRows - 1) / kDecodeRows;
+    out->min_tiles = kDecodeMinTiles;
+    out->workspace_bytes = decode_workspace(out->grid, d);
+    return ATTN_OK;
+}
+
+int attn_decode_trace(const int* seq_len, int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count,
+                      attn_decode_trace_entry* buf, size_t cap, size_t* n) {
+    if (!n || !seq_len) return fail(ATTN_ERR_INVALID_ARG, "seq_len and n must be non-null");
+    if (cap > 0 && !buf) return fail(ATTN_ERR_INVALID_ARG, "buf is null");
+    attn_decode_plan plan;
+    int rc = attn_decode_query_plan(B, H, kv_heads, d, opts, sm_count, &plan);
+    if (rc) return rc;
+    const int blocks = kv_heads * plan.head_blocks;
+    uint64_t total = 0;
+    for (int b = 0; b < B; ++b) {
+        if (seq_len[b] < 0) return fail(ATTN_ERR_INVALID_ARG, "a length is negative");
+        total += (uint64_t)decode_tiles(seq_len[b]) * blocks;
+    }
+    *n = 0;
+    if (total == 0) return ATTN_OK;
+    const int ctas = decode_ctas(total, plan.grid);
+    size_t count = 0;
+    uint64_t first = 0;     // the line's tiles before request b, block k
+    int cta = 0;
+    for (int b = 0; b < B; ++b) {
+        const int tiles = decode_tiles(seq_len[b]);
+        for (int k = 0; tiles > 0 && k < blocks; ++k, first += tiles) {
+            for (int t = 0; t < tiles;) {
+                while (decode_share_begin(total, ctas, cta + 1) <= first + t) ++cta;
+                const uint64_t share_end = decode_share_begin(total, ctas, cta + 1) - first;
+                const int end = share_end < (uint64_t)tiles ? (int)share_end : tiles;
+                if (count < cap) {
+                    attn_decode_trace_entry* e = &buf[count];
+                    e->cta = cta;
+                    e->request = b;
+                    e->kv_head = k / plan.head_blocks;
+                    e->head_block = k % plan.head_blocks;
+                    e->tile_begin = t;
+                    e->tile_end = end;
+                    e->n_tiles = tiles;
+                    e->part = t == 0 && end == tiles ? -1 : 2 * cta + (t == 0 ? 1 : 0);
+                    e->first_cta = decode_cta_of(total, ctas, first);
+                    e->last_cta = decode_cta_of(total, ctas, first + tiles - 1);
+                }
+                ++count;
+                t = end;
+            }
+        }
+    }
+    *n = count;
+    return ATTN_OK;
+}
+
+int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* block_table, long long table_stride, int max_pages,
+                      const int* seq_len, void* o, int B, int H, float scale, void* workspace, size_t workspace_bytes, void* stream,
+                      const attn_decode_opts* opts) {
+    attn_decode_opts z;
+    memset(&z, 0, sizeof(z));
+    if (opts) z = *opts;
+    attn_kv_cache c;
+    int rc = check_cache(cache, &c, false);
+    if (rc) return rc;
+    if ((rc = check_decode_shape(B, H, c.kv_heads, c.d, z))) return rc;
+    if (!block_table || !seq_len) return fail(ATTN_ERR_INVALID_ARG, "block_table and seq_len must be non-null");
+    if (max_pages < 1 || table_stride < 0 || !fits_address(table_stride, B)) return fail(ATTN_ERR_INVALID_ARG, "max_pages must be positive, table_stride not negative");
+    if (!std::isfinite(scale)) return fail(ATTN_ERR_INVALID_ARG, "scale must be finite");
+    if (((uintptr_t)block_table | (uintptr_t)seq_len | (uintptr_t)z.lse) & 3u) return fail(ATTN_ERR_ALIGNMENT, "block_table, seq_len and lse must be 4-byte aligned");
+    Region rq, ro;
+    if ((rc = rows_of("q", q, z.q_request, z.q_head, B, H, c.d, false, &rq)) || (rc = rows_of("o", o, z.o_request, z.o_head, B, H, c.d, true, &ro))) return rc;
+    if (!workspace || (uintptr_t)workspace & 15u)
+        return fail(workspace ? ATTN_ERR_ALIGNMENT : ATTN_ERR_INVALID_ARG, "the workspace must be non-null and 16-byte aligned");
+    DeviceState ds;
+    int dev = 0;
+    if ((rc = current_device(&ds, &dev))) return rc;
+    const int grid = decode_grid(ds.sm_count, z);
+    if (workspace_bytes < decode_workspace(grid, c.d)) return fail(ATTN_ERR_INVALID_ARG, "the workspace needs %zu bytes", decode_workspace(grid, c.d));
+    const Region ws = {workspace, 1, 0, 1, 0, (long long)decode_workspace(grid, c.d)};
+    const Region lse = {z.lse, 1, 0, 1, 0, (long long)B * H * 4};
+    const Region lens = {seq_len, 1, 0, 1, 0, (long long)B * 4}, table = {block_table, 1, 0, 1, 0, ((long long)(B - 1) * table_stride + max_pages) * 4};
+    const Region ins[] = {rq, span_of(c, c.k), span_of(c, c.v), lens, table};
+    const Region outs[] = {ro, lse, ws};
+    for (int i = 0; i < 3; ++i) {
+        for (const Region& in : ins)
+            if (overlap(outs[i], in)) return fail(ATTN_ERR_INVALID_ARG, "o, lse and the workspace must not overlap the inputs");
+        for (int j = i + 1; j < 3; ++j)
+            if (overlap(outs[i], outs[j])) return fail(ATTN_ERR_INVALID_ARG, "o, lse and the workspace must not overlap");
+    }
+    DecodeParams p;
+    const RopeTensor tq = in_of(rq);
+    p.q = tq.p; p.q_request = tq.token; p.q_head = tq.head;
+    const RopeOut to = out_of(ro);
+    p.o = to.p; p.o_request = to.token; p.o_head = to.head;
+    p.lse = z.lse;
+    p.cache = view_of(c);
+    p.table = block_table;
+    p.table_stride = table_stride;
+    p.seq_len = seq_len;
+    p.status = ds.status;
+    p.join = static_cast<int4*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(p.join + grid);
+    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * grid * kDecodeRows);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.B = B;
+    p.H = H;
+    p.kv_heads = c.kv_heads;
+    p.group = H / c.kv_heads;
+    p.head_blocks = (p.group + kDecodeRows - 1) / kDecodeRows;
+    const long long most = (long long)max_pages * c.page_size;
+    p.max_len = most < 2147483647ll ? (int)most : 2147483647;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (c.d == 128) rc = c.dtype == ATTN_BF16 ? launch_decode<128, 1>(dev, ds, p, grid, st) : launch_decode<128, 0>(dev, ds, p, grid, st);
+    else rc = c.dtype == ATTN_BF16 ? launch_decode<64, 1>(dev, ds, p, grid, st) : launch_decode<64, 0>(dev, ds, p, grid, st);
+    if (rc) return rc;
     return z.check_mode ? read_status(nullptr) : ATTN_OK;
 }
 

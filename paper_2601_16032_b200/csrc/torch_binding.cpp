@@ -1,0 +1,276 @@
+// The torch side of the entry points around the paged cache: takes tensors, checks what only a tensor knows (shapes, types,
+// devices, strides), allocates outputs that are not given, and calls the C ABI on the tensors' device and its current stream.
+//
+// Compiled, unlike the ctypes binding of the attention calls: these calls run for a few microseconds on the GPU and take
+// many small tensors, so what Python spends on looking each of them over would take several times as long as they do
+// (attn_page_plan: 31 us a call through ctypes and Python checks).  There is one path: without this module the wrappers raise.
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/extension.h>
+
+#include <optional>
+#include <string>
+
+#include "../../include/sawtooth_attn.h"
+
+namespace py = pybind11;
+using at::Tensor;
+using OptTensor = std::optional<Tensor>;
+
+namespace {
+
+struct Failure {
+    int status;
+    std::string message;
+};
+
+// Called with the message as a literal: nothing is built unless the check fails.
+inline void need(bool ok, const char* message) {
+    if (!ok) throw Failure{ATTN_ERR_INVALID_ARG, message};
+}
+inline void check(int status) {
+    if (status != ATTN_OK) {
+        const char* text = attn_last_error();
+        throw Failure{status, text && *text ? text : attn_status_string(status)};
+    }
+}
+
+void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
+
+int kind_of(const Tensor& t) {
+    if (t.scalar_type() == at::kBFloat16) return ATTN_BF16;
+    need(t.scalar_type() == at::kHalf, "tensors must be float16 or bfloat16");
+    return ATTN_F16;
+}
+
+// A contiguous tensor of one dimension with n elements of this type, on this device.
+template <typename T>
+T* vector_of(const Tensor& t, int64_t n, at::ScalarType type, const Tensor& like, const char* message) {
+    need(t.scalar_type() == type && t.device() == like.device() && t.dim() == 1 && t.numel() == n && t.is_contiguous(), message);
+    return static_cast<T*>(t.data_ptr());
+}
+
+struct Rows { void* p; long long outer, inner; };
+// A [outer, inner, d] tensor of q's type and device; its strides for the C ABI (both 0: contiguous).
+Rows rows_of(const Tensor& t, const Tensor& like, const char* message) {
+    need(t.dim() == 3 && t.scalar_type() == like.scalar_type() && t.device() == like.device(), message);
+    const int64_t n = t.size(0), h = t.size(1), d = t.size(2);
+    need(d <= 1 || t.stride(2) == 1, message);
+    long long a = t.stride(0), b = t.stride(1);
+    if (n <= 1) a = h > 1 ? 0 : h * d;
+    if (h <= 1) b = 0;
+    need(a != 0 || b != 0 || n * h <= 1, "a tensor must not be expanded over both of its outer dimensions");
+    return {t.data_ptr(), a, b};
+}
+
+attn_kv_cache cache_of(const Tensor& k, const Tensor& v, int layout, int64_t kv_heads, int64_t d, const Tensor& like) {
+    need(k.dim() == 4 && v.dim() == 4 && k.sizes() == v.sizes() && k.strides() == v.strides() && k.scalar_type() == like.scalar_type() &&
+             v.scalar_type() == like.scalar_type() && k.device() == like.device() && v.device() == like.device(),
+         "k_cache and v_cache must be alike: four dimensions, q's type and device, the same strides");
+    need(layout == ATTN_LAYOUT_BHND || layout == ATTN_LAYOUT_BNHD, "unknown layout");
+    const int token = layout == ATTN_LAYOUT_BNHD ? 1 : 2, head = 3 - token;
+    if (kv_heads < 0) kv_heads = k.size(head);
+    need(k.size(3) == d && k.size(head) == kv_heads && (d <= 1 || k.stride(3) == 1), "the cache must hold rows of d contiguous elements for all K/V heads");
+    need(k.size(token) <= 65536, "a page must not exceed 65536 tokens");
+    auto stride = [&](int i) { return k.size(i) <= 1 ? 0ll : (long long)k.stride(i); };
+    attn_kv_cache c = {};
+    c.k = k.data_ptr();
+    c.v = v.data_ptr();
+    c.num_pages = k.size(0);
+    c.page_stride = stride(0);
+    c.token_stride = stride(token);
+    c.head_stride = stride(head);
+    // Three strides of 0 say "contiguous" to the C ABI, which is what a cache of a single row is; an expanded one is not.
+    need(k.numel() == d || c.page_stride || c.token_stride || c.head_stride, "the cache must not be expanded");
+    c.page_size = (int)k.size(token);
+    c.kv_heads = (int)kv_heads;
+    c.d = (int)d;
+    c.dtype = kind_of(like);
+    c.layout = layout;
+    return c;
+}
+
+py::tuple page_plan(const Tensor& cached, const Tensor& added, int page_size, const Tensor& table, const Tensor& free_pages, const Tensor& free_count,
+                    int token_cap, const OptTensor& seq_len_out, const OptTensor& free_count_out) {
+    need(cached.is_cuda() && cached.dim() == 1, "cached must be a CUDA tensor of one dimension");
+    const int64_t B = cached.numel();
+    need(B >= 1 && B <= 8192, "there must be 1 to 8192 requests");
+    need(token_cap >= 0, "token_cap must not be negative");
+    need(table.dim() == 2 && table.scalar_type() == at::kInt && table.device() == cached.device() && table.size(0) == B && table.size(1) > 0 &&
+             table.size(1) <= 2147483647 && (table.size(1) == 1 || table.stride(1) == 1) && free_pages.numel() <= 2147483647,
+         "block_table must be an int32 tensor [B, width] on the device of the others with contiguous rows");
+    const c10::cuda::OptionalCUDAGuard guard(cached.device());
+    Tensor seq_len = seq_len_out ? *seq_len_out : at::empty_like(cached);
+    Tensor count_out = free_count_out ? *free_count_out : at::empty_like(free_count);
+    const auto options = cached.options();
+    Tensor q_start = at::empty({B + 1}, options), info = at::empty({4}, options), position = at::empty({token_cap}, options),
+           request = at::empty({token_cap}, options), slot = at::empty({token_cap}, options.dtype(at::kLong));
+    attn_page_pool pool = {};
+    pool.block_table = static_cast<int*>(table.data_ptr());
+    pool.table_stride = B > 1 ? table.stride(0) : table.size(1);
+    pool.free_pages = vector_of<int>(free_pages, free_pages.numel(), at::kInt, cached, "free_pages must be a contiguous int32 tensor on the device of the others");
+    pool.free_count = vector_of<int>(free_count, 1, at::kInt, cached, "free_count must be an int32 tensor [1] on the device of the others");
+    pool.free_count_out = vector_of<int>(count_out, 1, at::kInt, cached, "free_count_out must be an int32 tensor [1] on the device of the others");
+    pool.width = (int)table.size(1);
+    pool.capacity = (int)free_pages.numel();
+    pool.page_size = page_size;
+    check(attn_page_plan(&pool, vector_of<int>(cached, B, at::kInt, cached, "cached must be a contiguous int32 tensor"),
+                         vector_of<int>(added, B, at::kInt, cached, "added must be a contiguous int32 tensor like cached"), (int)B,
+                         vector_of<int>(seq_len, B, at::kInt, cached, "seq_len must be a contiguous int32 tensor like cached"), q_start.data_ptr<int>(),
+                         reinterpret_cast<long long*>(slot.data_ptr()), position.data_ptr<int>(), request.data_ptr<int>(), token_cap, info.data_ptr<int>(),
+                         stream_of(cached)));
+    return py::make_tuple(seq_len, q_start, slot, position, request, count_out, info);
+}
+
+// What the norm and the rotation take in both directions.
+struct RopeArgs {
+    const void *q_weight = nullptr, *k_weight = nullptr;
+    const int* position = nullptr;
+    const double* inv_freq = nullptr;
+    int rot = 0, f32 = 0;
+    RopeArgs(const Tensor& q, const OptTensor& wq, const OptTensor& wk, const OptTensor& pos, const OptTensor& freq) {
+        const int64_t T = q.size(0), d = q.size(2);
+        f32 = (wq && wq->scalar_type() == at::kFloat) || (wk && wk->scalar_type() == at::kFloat);
+        const at::ScalarType type = f32 ? at::kFloat : q.scalar_type();
+        if (wq) q_weight = vector_of<void>(*wq, d, type, q, "weights must be contiguous tensors [d], both float32 or both of q's type, on q's device");
+        if (wk) k_weight = vector_of<void>(*wk, d, type, q, "weights must be contiguous tensors [d], both float32 or both of q's type, on q's device");
+        if (freq) {
+            need(pos.has_value(), "a rotation needs position");
+            position = vector_of<int>(*pos, T, at::kInt, q, "position must be a contiguous int32 tensor [T] on q's device");
+            need(freq->numel() <= d / 2, "inv_freq must have at most d / 2 elements");
+            inv_freq = vector_of<double>(*freq, freq->numel(), at::kDouble, q, "inv_freq must be a contiguous float64 tensor [rot_dim / 2] on q's device");
+            rot = 2 * (int)freq->numel();
+        }
+    }
+};
+
+void check_qk(const Tensor& q, const Tensor& k) {
+    need(q.is_cuda() && q.dim() == 3 && k.dim() == 3 && k.size(0) == q.size(0) && k.size(2) == q.size(2), "q must be a CUDA tensor [T, H, d], k one of [T, kv_heads, d]");
+    need(q.size(0) <= (1 << 30) && q.size(1) <= 65536 && k.size(1) <= 65536 && q.size(2) <= 65536, "q or k is too large");
+}
+
+py::tuple qk_norm_rope(const Tensor& q, const Tensor& k, const OptTensor& v, const OptTensor& q_weight, const OptTensor& k_weight, double eps,
+                       const OptTensor& position, const OptTensor& inv_freq, bool interleaved, const OptTensor& k_cache, const OptTensor& v_cache, int layout,
+                       const OptTensor& slot, const OptTensor& q_out_given, const OptTensor& k_out_given) {
+    check_qk(q, k);
+    const bool cached = k_cache.has_value();
+    need(v_cache.has_value() == cached && slot.has_value() == cached && v.has_value() == cached, "k_cache, v_cache, slot and v go together");
+    const c10::cuda::OptionalCUDAGuard guard(q.device());
+    const RopeArgs a(q, q_weight, k_weight, position, inv_freq);
+    Tensor q_out = q_out_given ? *q_out_given : at::empty(q.sizes(), q.options());
+    OptTensor k_out = k_out_given;
+    if (!k_out && !cached) k_out = at::empty(k.sizes(), k.options());
+    need(q_out.sizes() == q.sizes() && (!k_out || k_out->sizes() == k.sizes()) && (!v || v->sizes() == k.sizes()), "v, q_out and k_out must have the shapes of k, q and k");
+    attn_rope_opts o = {};
+    const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), rk = rows_of(k, q, "k must be like q: type, device, rows of d contiguous elements"),
+               rqo = rows_of(q_out, q, "q_out must be like q: type, device, rows of d contiguous elements");
+    Rows rv = {}, rko = {};
+    if (k_out) rko = rows_of(*k_out, q, "k_out must be like q: type, device, rows of d contiguous elements");
+    o.q_token = rq.outer; o.q_head = rq.inner; o.k_token = rk.outer; o.k_head = rk.inner;
+    o.q_out_token = rqo.outer; o.q_out_head = rqo.inner; o.k_out_token = rko.outer; o.k_out_head = rko.inner;
+    o.weight_f32 = a.f32;
+    attn_kv_cache cache;
+    if (cached) {
+        rv = rows_of(*v, q, "v must be like q: type, device, rows of d contiguous elements");
+        o.v_token = rv.outer; o.v_head = rv.inner;
+        cache = cache_of(*k_cache, *v_cache, layout, k.size(1), k.size(2), q);
+        o.cache = &cache;
+        o.slot = vector_of<long long>(*slot, q.size(0), at::kLong, q, "slot must be a contiguous int64 tensor [T] on q's device");
+    }
+    if (q.size(0) > 0)
+        check(attn_qk_norm_rope(rq.p, rk.p, rv.p, rqo.p, rko.p, (int)q.size(0), (int)q.size(1), (int)k.size(1), (int)q.size(2), kind_of(q), a.q_weight,
+                                a.k_weight, (float)eps, a.position, a.inv_freq, a.rot, interleaved ? ATTN_ROPE_ADJACENT : ATTN_ROPE_HALVES, stream_of(q), &o));
+    return py::make_tuple(q_out, k_out);
+}
+
+// The caller's workspace, or a new one; its size is checked by the C ABI.
+Tensor workspace_of(const OptTensor& given, size_t bytes, const Tensor& like) {
+    if (!given) return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+    need(given->device() == like.device() && given->is_contiguous(), "the workspace must be a contiguous tensor on q's device");
+    return *given;
+}
+
+py::tuple qk_norm_rope_backward(const Tensor& dq_out, const Tensor& dk_out, const Tensor& q, const Tensor& k, const OptTensor& q_weight, const OptTensor& k_weight,
+                                double eps, const OptTensor& position, const OptTensor& inv_freq, bool interleaved, const OptTensor& dq_given,
+                                const OptTensor& dk_given, const OptTensor& workspace_given) {
+    check_qk(q, k);
+    const c10::cuda::OptionalCUDAGuard guard(q.device());
+    const RopeArgs a(q, q_weight, k_weight, position, inv_freq);
+    Tensor dq = dq_given ? *dq_given : at::empty(q.sizes(), q.options()), dk = dk_given ? *dk_given : at::empty(k.sizes(), k.options());
+    need(dq.sizes() == q.sizes() && dq_out.sizes() == q.sizes() && dk.sizes() == k.sizes() && dk_out.sizes() == k.sizes(), "gradients must have the shapes of q and k");
+    OptTensor dq_weight, dk_weight;
+    if (a.q_weight) dq_weight = at::empty({q.size(2)}, q.options().dtype(at::kFloat));
+    if (a.k_weight) dk_weight = at::empty({q.size(2)}, q.options().dtype(at::kFloat));
+    Tensor workspace = workspace_of(workspace_given, attn_rope_bwd_workspace_bytes((int)q.size(2)), q);
+    attn_rope_opts o = {};
+    const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), rk = rows_of(k, q, "k must be like q: type, device, rows of d contiguous elements"),
+               gq = rows_of(dq_out, q, "dq_out must be like q: type, device, rows of d contiguous elements"),
+               gk = rows_of(dk_out, q, "dk_out must be like q: type, device, rows of d contiguous elements"),
+               rdq = rows_of(dq, q, "dq must be like q: type, device, rows of d contiguous elements"),
+               rdk = rows_of(dk, q, "dk must be like q: type, device, rows of d contiguous elements");
+    o.q_token = rq.outer; o.q_head = rq.inner; o.k_token = rk.outer; o.k_head = rk.inner;
+    o.q_out_token = gq.outer; o.q_out_head = gq.inner; o.k_out_token = gk.outer; o.k_out_head = gk.inner;
+    o.dq_token = rdq.outer; o.dq_head = rdq.inner; o.dk_token = rdk.outer; o.dk_head = rdk.inner;
+    o.weight_f32 = a.f32;
+    if (q.size(0) == 0) {
+        if (dq_weight) dq_weight->zero_();
+        if (dk_weight) dk_weight->zero_();
+    } else {
+        check(attn_qk_norm_rope_bwd(gq.p, gk.p, rq.p, rk.p, rdq.p, rdk.p, dq_weight ? dq_weight->data_ptr<float>() : nullptr,
+                                    dk_weight ? dk_weight->data_ptr<float>() : nullptr, (int)q.size(0), (int)q.size(1), (int)k.size(1), (int)q.size(2), kind_of(q),
+                                    a.q_weight, a.k_weight, (float)eps, a.position, a.inv_freq, a.rot, interleaved ? ATTN_ROPE_ADJACENT : ATTN_ROPE_HALVES,
+                                    workspace.data_ptr(), workspace.nbytes(), stream_of(q), &o));
+    }
+    return py::make_tuple(dq, dk, dq_weight, dk_weight);
+}
+
+py::tuple decode_paged(const Tensor& q, const Tensor& k_cache, const Tensor& v_cache, const Tensor& table, const Tensor& seq_len, std::optional<double> scale,
+                       int layout, bool return_lse, const OptTensor& out, const OptTensor& workspace_given, int max_ctas) {
+    need(q.is_cuda() && q.dim() == 3 && q.size(0) <= 2147483647 && q.size(1) <= 65536 && q.size(2) <= 65536, "q must be a CUDA tensor [B, H, d]");
+    const int64_t B = q.size(0), H = q.size(1), d = q.size(2);
+    const c10::cuda::OptionalCUDAGuard guard(q.device());
+    need(table.dim() == 2 && table.scalar_type() == at::kInt && table.device() == q.device() && table.size(0) == B && table.size(1) > 0 &&
+             table.size(1) <= 2147483647 && (table.size(1) == 1 || table.stride(1) == 1),
+         "block_table must be an int32 tensor [B, max_pages] on q's device with contiguous rows");
+    Tensor o = out ? *out : at::empty(q.sizes(), q.options());
+    need(o.sizes() == q.sizes(), "out must have q's shape");
+    OptTensor lse;
+    if (return_lse) lse = at::empty({B, H}, q.options().dtype(at::kFloat));
+    if (B == 0) return py::make_tuple(o, lse);
+    const attn_kv_cache cache = cache_of(k_cache, v_cache, layout, -1, d, q);
+    const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), ro = rows_of(o, q, "out must be like q: type, device, rows of d contiguous elements");
+    attn_decode_opts opts = {};
+    opts.q_request = rq.outer; opts.q_head = rq.inner; opts.o_request = ro.outer; opts.o_head = ro.inner;
+    opts.lse = lse ? lse->data_ptr<float>() : nullptr;
+    opts.max_ctas = max_ctas;
+    size_t bytes = 0;
+    if (!workspace_given) {
+        attn_decode_plan plan;
+        check(attn_decode_query_plan((int)B, (int)H, cache.kv_heads, (int)d, &opts, 0, &plan));
+        bytes = plan.workspace_bytes;
+    }
+    Tensor workspace = workspace_of(workspace_given, bytes, q);
+    check(attn_decode_paged(rq.p, &cache, static_cast<const int*>(table.data_ptr()), B > 1 ? table.stride(0) : table.size(1), (int)table.size(1),
+                            vector_of<int>(seq_len, B, at::kInt, q, "seq_len must be a contiguous int32 tensor [B] on q's device"), ro.p, (int)B, (int)H,
+                            (float)(scale ? *scale : 1.0 / std::sqrt((double)d)), workspace.data_ptr(), workspace.nbytes(), stream_of(q), &opts));
+    return py::make_tuple(o, lse);
+}
+
+PyObject* error_class = nullptr;   // AttnError(status, message)
+
+}  // namespace
+
+PYBIND11_MODULE(_torch_binding, m) {
+    py::register_exception_translator([](std::exception_ptr p) {
+        try {
+            if (p) std::rethrow_exception(p);
+        } catch (const Failure& f) {
+            PyErr_SetObject(error_class ? error_class : PyExc_RuntimeError, py::make_tuple(f.status, f.message).ptr());
+        }
+    });
+    m.def("set_error_class", [](py::object c) { error_class = c.release().ptr(); });
+    m.def("page_plan", &page_plan);
+    m.def("qk_norm_rope", &qk_norm_rope);
+    m.def("qk_norm_rope_backward", &qk_norm_rope_backward);
+    m.def("decode_paged", &decode_paged);
+}

@@ -100,6 +100,29 @@ def test_rope_backward(change, status):
     refused(rope_call(backward=True, **change), status)
 
 
+def decode_call(cache=None, opts=None, **change):
+    a = dict(q=at(0), table=at(1), stride=64, pages=64, lens=at(2), o=at(3), B=4, H=8, scale=0.1, ws=at(4), ws_bytes=1 << 26)
+    a.update(change)
+    c = dict(k=at(14), v=at(15), num_pages=100, page_size=16, kv_heads=2, d=128, dtype=sa.BF16)
+    c.update(cache or {})
+    o = sa.DecodeOpts()
+    for name, value in (opts or {}).items():
+        setattr(o, name, value)
+    return lambda: sa.attn_decode_paged(a["q"], sa.KVCache(**c), a["table"], a["stride"], a["pages"], a["lens"], a["o"], a["B"], a["H"], a["scale"], a["ws"],
+                                        a["ws_bytes"], 0, o)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(q=0), -1), (dict(table=0), -1), (dict(lens=0), -1), (dict(o=0), -1), (dict(ws=0), -1), (dict(ws=at(4) + 8), -3), (dict(B=0), -1), (dict(H=7), -1),
+    (dict(H=0), -1), (dict(pages=0), -1), (dict(stride=-1), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(q=at(0) + 4), -3),
+    (dict(lens=at(2) + 2), -3), (dict(opts=dict(lse=at(5) + 2)), -3), (dict(opts=dict(max_ctas=-1)), -1), (dict(opts=dict(check_mode=2)), -1),
+    (dict(opts=dict(q_head=4)), -1), (dict(opts=dict(o_request=64, o_head=128)), -1), (dict(cache=dict(d=80)), -2), (dict(cache=dict(k=0)), -1),
+    (dict(cache=dict(v=at(14))), -1), (dict(cache=dict(page_size=0)), -1), (dict(cache=dict(kv_heads=3)), -1), (dict(cache=dict(dtype=4)), -1),
+    (dict(cache=dict(k=at(14) + 8)), -3), (dict(cache=dict(page_stride=4, token_stride=8, head_stride=8)), -1)])
+def test_decode(change, status):
+    refused(decode_call(**change), status)
+
+
 def test_queries_and_keys_may_lie_side_by_side():
     """Interleaved parts of one array do not overlap: the call gets as far as looking for a device."""
     import torch
@@ -113,6 +136,7 @@ def test_queries_and_keys_may_lie_side_by_side():
     refused(rope_call(backward=True), -4)
     refused(rope_call(cache={}, v=at(2), opts=dict(slot=at(16))), -4)
     refused(plan_call(seq_len=at(4), count_out=at(2), position=0, request=0), -4)
+    refused(decode_call(), -4)
 
 
 def test_status_of_an_index_out_of_range_has_a_text():
