@@ -374,7 +374,7 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
  * whatever they are.  A length below 0 or above max_pages * page_size is cut to that range, a page number outside [0, num_pages) reads
  * as zeros; both are noted in the status word and that request's o is then of no use.
  *
- * The work is cut over the length: the 64-token tiles of all requests and K/V heads, in that order, are dealt out to the CTAs in equal
+ * The work is cut over the length: the tiles (64 tokens; 128 at d = 64) of all requests and K/V heads, in that order, are dealt out to the CTAs in equal
  * contiguous shares whatever the lengths (attn_decode_trace replays it), and requests cut by a share's border are joined by
  * their running maxima and sums.  For fixed arguments bitwise reproducible.  The products take their 16-bit operands as they are;
  * probabilities enter the second product as the sum of two 16-bit numbers; sums are fp32; o is rounded once.
@@ -394,7 +394,7 @@ typedef struct {
 typedef struct {
     int grid, threads, smem_bytes;
     int tile_tokens;         /* tokens of a tile */
-    int head_blocks;         /* blocks of up to 16 query heads that read one K/V head */
+    int head_blocks;         /* blocks of up to 32 query heads that read one K/V head */
     int min_tiles;           /* a CTA's share is at least this many tiles (but for rounding) */
     size_t workspace_bytes;
 } attn_decode_plan;

@@ -2,16 +2,20 @@
 // split evenly over the CTAs along the lengths (decode_schedule.h), and a second, short kernel that joins what the split cut.
 //
 // What bounds it is reading K and V once: per K/V head and token 4 d bytes against 4 d multiply-adds per query head.  So
-// the layout serves the loads.  Each warp streams its own 16 tokens of every 64-token tile through a ring of its own in shared
-// memory with 16-byte asynchronous copies (any page size and any strides; no barrier between warps in the loop), page numbers
-// are looked up one tile ahead, and the loads run across the borders of requests.  The products have as many rows as query heads
-// share a K/V head, 16 at most: a warp's mma.sync tile (m16n8k16), with the queries in registers.  A 128-row tcgen05 tile would be
-// mostly padding, and its trips through tensor memory would add to the latency of short calls, where the kernel is bound by the
-// chain of one tile.
+// the layout serves the loads.  Each warp streams a quarter of every tile through a ring in shared memory with 16-byte asynchronous
+// copies (any page size and any strides), page numbers are looked up one tile ahead, and the loads run across the borders of requests.
+//
+// The products are kept in the transposed form S^T = K Q^T, O^T = V^T P^T, with tokens (then dimensions) as the 16 rows of an
+// mma.sync m16n8k16 and query heads as its 8 columns, so that up to 8 heads cost half of what they would as rows.  Turning P
+// round between the products takes a movmatrix per 8 x 8 block.  A warp works for 8 heads; where 9 to 16 or 17 to 32 share a K/V head, two
+// or four warps form a group that pools its tokens: each reads all of them for its own 8 heads, which leaves fewer sums to add up
+// at the end of a request (none for four) and keeps every warp's accumulators at d / 16 blocks.  A 128-row tcgen05 tile would be as well filled in this form,
+// but the products are not what bounds the kernel, and the way through tensor memory would add to the latency of short calls.
 //
 // Probabilities enter the second product as the sum of two 16-bit numbers, p = hi + lo, so that rounding them adds nothing to the one
-// rounding of the result (a single bf16 would add as much again); they are taken relative to the running maximum, for fp16
-// times 2^kBias, so that small ones keep clear of its subnormal numbers.
+// rounding of the result (a single 16-bit p would add as much again).  They are taken relative to a reference that follows the
+// running maximum only when it has been passed by more than 2^8 (p and its sum always share one reference, so this is exact), for
+// fp16 times 2^7, so that they stay below 2^15 and small ones keep clear of the subnormal numbers.
 #pragma once
 #include "decode_schedule.h"
 #include "paged_common.cuh"
@@ -28,23 +32,26 @@ struct DecodeParams {
     long long table_stride;
     const int* seq_len;
     int* status;
-    int4* join;              // [grid] {parts, request, head block index, 0} of the request cut in that CTA's share
-    float2* part_ml;         // [2 grid][16] running maximum (log2 units) and sum
-    float* part_o;           // [2 grid][16][d] sums
+    int4* join;              // [2 grid] {parts, first CTA, request, head block index} of the results that a CTA's head (2 c) and
+                             // tail (2 c + 1) pieces are parts of; parts = 0: none
+    float2* part_ml;         // [2 grid][rows] reference (log2 units) and sum
+    float* part_o;           // [2 grid][rows][d] sums
     float scale_log2;
     int B, H, kv_heads, group, head_blocks, max_len;
 };
 
 constexpr int kDecodeThreads = 128;
 constexpr int kDecodeWarps = 4;
-constexpr int kDecodeWarpTokens = kDecodeTile / kDecodeWarps;   // 16
+constexpr float kDecodeSlack = 8.f;   // log2 units by which scores may pass the reference
 
 template <int kD>
 struct DecodeGeometry {
+    static constexpr int kTile = decode_tile(kD);
+    static constexpr int kWarpTokens = kTile / kDecodeWarps;                   // 16 or 32
     static constexpr int kRowBytes = kD * 2;
-    static constexpr int kStageBytes = 2 * kDecodeWarpTokens * kRowBytes;      // K and V of a warp's tokens; also 16 fp32 rows of d
-    static constexpr int kStages = kD == 128 ? 3 : 6;
-    static constexpr int kSmem = kDecodeWarps * kStages * kStageBytes;          // 96 KiB: two CTAs an SM
+    static constexpr int kStageBytes = 2 * kWarpTokens * kRowBytes;            // K and V of a warp's tokens: 8 KiB
+    static constexpr int kStages = 2;
+    static constexpr int kSmem = kDecodeWarps * kStages * kStageBytes;          // 64 KiB: three CTAs an SM
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes)   // copies `bytes` (16 or 0), zero-fills the rest
@@ -57,33 +64,37 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 template <int kBf16>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     if (kBf16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)   // of 16-bit elements, two to a lane
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 // A request's length, cut to what its table row can hold.
-__device__ __forceinline__ int decode_len(const DecodeParams& p, int b)
-{
-    const int len = p.seq_len[b];
-    return len < 0 ? 0 : len > p.max_len ? p.max_len : len;
-}
+__device__ __forceinline__ int decode_cut(const DecodeParams& p, int len) { return len < 0 ? 0 : len > p.max_len ? p.max_len : len; }
 
 // A place in the line of tiles: tile `tile` of n of the head block `block` of request b.
+template <int kTile>
 struct DecodeCursor {
-    int b, block, tile, n, len, next_len;   // next_len: the length of request b + 1, read ahead
+    int b, block, tile, n, len, next_raw;   // next_raw: the length of request b + 1 as stored, read ahead (and not touched until needed)
     __device__ __forceinline__ void advance(const DecodeParams& p, int blocks)
     {
         if (++tile < n) return;
@@ -92,35 +103,44 @@ struct DecodeCursor {
         block = 0;
         do {
             ++b;
-            len = next_len;
-            next_len = b + 1 < p.B ? decode_len(p, b + 1) : 0;
+            len = decode_cut(p, next_raw);
+            next_raw = b + 1 < p.B ? p.seq_len[b + 1] : 0;
         } while (len == 0 && b < p.B);
-        n = decode_tiles(len);
+        n = decode_tiles(len, kTile);
     }
 };
 
-template <int kD, int kBf16>
-__global__ void __launch_bounds__(kDecodeThreads, 2) decode_paged_kernel(const DecodeParams p)
+// kN: warps of a group, and blocks of 8 query heads.
+template <int kD, int kBf16, int kN>
+__global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const DecodeParams p)
 {
     using G = DecodeGeometry<kD>;
     constexpr int kStages = G::kStages, kPieces = kD / 8;            // 16-byte pieces of a row
-    constexpr float kBias = kBf16 ? 0.f : 15.f;                      // log2 of the factor on the probabilities
+    constexpr int kRows = 8 * kN, kGroups = kDecodeWarps / kN;       // query heads of a block; groups of warps
+    constexpr int kGroupTokens = kN * G::kWarpTokens;                // tokens of a tile that a group looks after
+    constexpr int kM = kGroupTokens >= 32 ? 2 : 1;                   // blocks of 16 tokens worked on at a time
+    constexpr float kBias = kBf16 ? 0.f : 7.f;                       // log2 of the factor on the probabilities
     extern __shared__ __align__(128) uint8_t decode_smem[];
-    __shared__ float2 warp_ml[kDecodeWarps][kDecodeRows];
+    __shared__ float2 warp_ml[kDecodeWarps][8];
     __shared__ uint64_t scan[kDecodeWarps];
-    __shared__ int start_at[2];
+    __shared__ int start_at;
     __shared__ uint64_t start_off;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int group = warp / kN, member = warp % kN;
     const int blocks = p.kv_heads * p.head_blocks;
+    auto group_sync = [&]() {
+        if (kN == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kN) : "memory");
+    };
 
     // ---- this CTA's share: sum of all requests' tiles, then the request and tile the share begins with
-    const int chunk = (p.B + kDecodeThreads - 1) / kDecodeThreads, b_lo = tid * chunk, b_hi = min(p.B, b_lo + chunk);
+    const int chunk = (p.B + kDecodeThreads - 1) / kDecodeThreads, b_lo = min(p.B, tid * chunk), b_hi = min(p.B, b_lo + chunk);
     uint64_t mine = 0;
     bool bad = false;
     for (int b = b_lo; b < b_hi; ++b) {
         const int raw = p.seq_len[b];
         bad |= raw < 0 || raw > p.max_len;
-        mine += (uint64_t)decode_tiles(raw < 0 ? 0 : raw > p.max_len ? p.max_len : raw) * blocks;
+        mine += (uint64_t)decode_tiles(decode_cut(p, raw), G::kTile) * blocks;
     }
     if (bad && blockIdx.x == 0) note_index(p.status, kIndexLength);
     uint64_t upto = mine;
@@ -139,62 +159,90 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_paged_kernel(const D
     }
     const int ctas = decode_ctas(total, gridDim.x), cta = blockIdx.x;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int4 join = make_int4(0, 0, 0, 0);
+    int joins = 0;     // bit i: entry 2 cta + i of p.join is written
     if (cta < ctas) {
-        const uint64_t begin = decode_share_begin(total, ctas, cta);
-        int left = (int)(decode_share_begin(total, ctas, cta + 1) - begin);
+        const uint64_t begin = decode_share_begin(total, ctas, cta), end = decode_share_begin(total, ctas, cta + 1);
+        int left = (int)(end - begin);
         if (begin >= upto - mine && begin < upto) {
             uint64_t at = begin - (upto - mine);
             int b = b_lo;
             for (;; ++b) {
-                const uint64_t t = (uint64_t)decode_tiles(decode_len(p, b)) * blocks;
+                const uint64_t t = (uint64_t)decode_tiles(decode_cut(p, p.seq_len[b]), G::kTile) * blocks;
                 if (at < t) break;
                 at -= t;
             }
-            start_at[0] = b;
+            start_at = b;
             start_off = at;
         }
         __syncthreads();
-        DecodeCursor ld;
-        ld.b = start_at[0];
-        ld.len = decode_len(p, ld.b);
-        ld.next_len = ld.b + 1 < p.B ? decode_len(p, ld.b + 1) : 0;
-        ld.n = decode_tiles(ld.len);
-        ld.block = (int)(start_off / (uint64_t)ld.n);
-        ld.tile = (int)(start_off % (uint64_t)ld.n);
-        DecodeCursor cp = ld;
+        DecodeCursor<G::kTile> ld;
+        ld.b = start_at;
+        ld.len = decode_cut(p, p.seq_len[ld.b]);
+        ld.next_raw = ld.b + 1 < p.B ? p.seq_len[ld.b + 1] : 0;
+        ld.n = decode_tiles(ld.len, G::kTile);
+        ld.block = (int)decode_div(start_off, (uint64_t)ld.n);
+        ld.tile = (int)(start_off - (uint64_t)ld.block * (uint64_t)ld.n);
+        DecodeCursor<G::kTile> cp = ld;
         int to_load = left;
 
-        const uint32_t ring = ptx::smem_u32(decode_smem) + warp * kStages * G::kStageBytes;
-        // The page of the token that lane l < 16 looks after, in the tile the load cursor is at.
+        // A group's stage: K rows of its tokens, then V rows.
+        constexpr int kGroupStage = kN * G::kStageBytes;
+        uint8_t* const ring_p = decode_smem + (size_t)group * kStages * kGroupStage;
+        const uint32_t ring = ptx::smem_u32(ring_p);
+        // The page of the token that this lane looks after, in the tile the load cursor is at.
+        const int my_token = warp * G::kWarpTokens + lane % G::kWarpTokens;
         auto look_up = [&]() -> int {
-            const int token = ld.tile * kDecodeTile + warp * kDecodeWarpTokens + (lane & 15);
+            const int token = ld.tile * G::kTile + my_token;
             return to_load > 0 && token < ld.len ? p.table[(long long)ld.b * p.table_stride + p.cache.page.div((uint32_t)token)] : -1;
         };
         int page = look_up();
+        constexpr int kRowsAtOnce = 32 / kPieces;       // rows that a warp's copy instruction covers
+        const int piece = lane % kPieces, row0 = lane / kPieces;
+        const uint32_t dst0 = ring + member * G::kWarpTokens * G::kRowBytes;
+        const bool runs = p.cache.page.d % 16 == 0;      // 16 tokens from a multiple of 16 on lie in one page
+        const long long lane_off = row0 * p.cache.token_stride + piece * 8, step = kRowsAtOnce * p.cache.token_stride;
         auto issue = [&](int stage) {
             if (to_load > 0) {
-                const int token = ld.tile * kDecodeTile + warp * kDecodeWarpTokens + (lane & 15);
-                const bool there = token < ld.len;
+                const int token = ld.tile * G::kTile + my_token;
                 long long at = -1;
-                if (there) {
+                if (token < ld.len) {
                     if (page >= 0 && page < p.cache.num_pages)
                         at = page * p.cache.page_stride + (long long)(token - (int)p.cache.page.div((uint32_t)token) * (int)p.cache.page.d) * p.cache.token_stride +
                              (long long)(ld.block / p.head_blocks) * p.cache.head_stride;
                     else
                         note_index(p.status, kIndexPage);
                 }
-                constexpr int kRowsAtOnce = 32 / kPieces;
-                const uint32_t k_dst = ring + stage * G::kStageBytes, v_dst = k_dst + kDecodeWarpTokens * G::kRowBytes;
-                const int piece = lane % kPieces;
+                const uint32_t k_dst = dst0 + stage * kGroupStage, v_dst = k_dst + kGroupTokens * G::kRowBytes;
+                if (runs) {
+                    // One page for each 16 rows: the address of the first, and equal steps from row to row.  (The general way below
+                    // takes 30 % more of a warp's instructions in the loop.)
 #pragma unroll
-                for (int i = 0; i < kDecodeWarpTokens / kRowsAtOnce; ++i) {
-                    const int row = i * kRowsAtOnce + lane / kPieces;
-                    const long long off = __shfl_sync(0xffffffffu, at, row);
-                    const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
-                    const long long from = (off < 0 ? 0 : off) + piece * 8;
-                    cp_async16(k_dst + d, p.cache.k + from, off < 0 ? 0 : 16);
-                    cp_async16(v_dst + d, p.cache.v + from, off < 0 ? 0 : 16);
+                    for (int half = 0; half < G::kWarpTokens / 16; ++half) {
+                        const long long base = __shfl_sync(0xffffffffu, at, 16 * half);
+                        const int rows = base < 0 ? 0 : min(16, ld.len - ld.tile * G::kTile - warp * G::kWarpTokens - 16 * half);
+                        const uint16_t* k_from = p.cache.k + (base < 0 ? 0 : base + lane_off);
+                        const uint16_t* v_from = p.cache.v + (base < 0 ? 0 : base + lane_off);
+#pragma unroll
+                        for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                            const int row = 16 * half + i * kRowsAtOnce + row0;
+                            const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
+                            const bool there = i * kRowsAtOnce + row0 < rows;
+                            cp_async16(k_dst + d, there ? k_from : p.cache.k, there ? 16 : 0);
+                            cp_async16(v_dst + d, there ? v_from : p.cache.v, there ? 16 : 0);
+                            k_from += step;
+                            v_from += step;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < G::kWarpTokens / kRowsAtOnce; ++i) {
+                        const int row = i * kRowsAtOnce + row0;
+                        const long long off = __shfl_sync(0xffffffffu, at, row);
+                        const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
+                        const long long from = off < 0 ? 0 : off + piece * 8;
+                        cp_async16(k_dst + d, p.cache.k + from, off < 0 ? 0 : 16);
+                        cp_async16(v_dst + d, p.cache.v + from, off < 0 ? 0 : 16);
+                    }
                 }
                 --to_load;
                 if (to_load > 0) ld.advance(p, blocks);
@@ -203,161 +251,186 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_paged_kernel(const D
             cp_async_commit();
         };
 
-        uint32_t qf[kD / 16][4];
+        uint32_t qf[kD / 16][2];              // Q^T as the B operand: dimensions x heads
         auto load_q = [&]() {
-            const int kvh = cp.block / p.head_blocks, first = (cp.block % p.head_blocks) * kDecodeRows;
-            const int rows = min(kDecodeRows, p.group - first);
-            const uint16_t* base = p.q + (long long)cp.b * p.q_request + (long long)(kvh * p.group + first) * p.q_head + 2 * (lane & 3);
-            const int r0 = lane >> 2, r1 = r0 + 8;
+            const int kvh = cp.block / p.head_blocks, row = (cp.block % p.head_blocks) * kRows + 8 * member + (lane >> 2);
+            const bool there = row < p.group;
+            const uint16_t* from = p.q + (long long)cp.b * p.q_request + (long long)(kvh * p.group + row) * p.q_head + 2 * (lane & 3);
 #pragma unroll
             for (int kk = 0; kk < kD / 16; ++kk) {
-                qf[kk][0] = r0 < rows ? *reinterpret_cast<const uint32_t*>(base + r0 * p.q_head + kk * 16) : 0u;
-                qf[kk][1] = r1 < rows ? *reinterpret_cast<const uint32_t*>(base + r1 * p.q_head + kk * 16) : 0u;
-                qf[kk][2] = r0 < rows ? *reinterpret_cast<const uint32_t*>(base + r0 * p.q_head + kk * 16 + 8) : 0u;
-                qf[kk][3] = r1 < rows ? *reinterpret_cast<const uint32_t*>(base + r1 * p.q_head + kk * 16 + 8) : 0u;
+                qf[kk][0] = there ? *reinterpret_cast<const uint32_t*>(from + kk * 16) : 0u;
+                qf[kk][1] = there ? *reinterpret_cast<const uint32_t*>(from + kk * 16 + 8) : 0u;
             }
         };
 
 #pragma unroll
         for (int s = 0; s < kStages - 1; ++s) issue(s);
         load_q();
-        float acc[kD / 8][4] = {};
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float acc[kD / 16][4];                // O^T: 16 dimensions x 8 heads a block; this lane's columns are heads 2 (lane & 3) and the next
+        float ref[2], l[2];                   // of those heads: the reference of the exponents, and this lane's share of the sum
+        auto clear = [&]() {
+            ref[0] = ref[1] = -INFINITY;
+            l[0] = l[1] = 0.f;
+#pragma unroll
+            for (int j = 0; j < kD / 16; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+        };
+        clear();
         int stage = 0, first_tile = cp.tile;
-        // ldmatrix: the row and piece that this lane gives the address of, for K (tokens are columns of B) and V (tokens are its rows)
-        const int k_row = (lane & 7) + ((lane >> 4) << 3), k_half = (lane >> 3) & 1;
-        const int v_row = (lane & 7) + (((lane >> 3) & 1) << 3), v_half = lane >> 4;
+        // ldmatrix: the row and piece that this lane gives the address of.  K as A operand (tokens x dimensions): blocks in the order tokens
+        // 0-7 and 8-15, then the next 8 dimensions; V transposed (dimensions x tokens): dimensions 0-7 and 8-15, then the next 8 tokens.
+        const int k_row = lane & 15, k_half = lane >> 4;
+        const int v_row = (lane & 7) + ((lane >> 4) << 3), v_half = (lane >> 3) & 1;
 
         for (; left > 0; --left) {
             cp_async_wait<kStages - 2>();
-            __syncwarp();
+            group_sync();
             issue(stage == 0 ? kStages - 1 : stage - 1);
-            const uint32_t k_base = ring + stage * G::kStageBytes, v_base = k_base + kDecodeWarpTokens * G::kRowBytes;
-            const int valid = cp.len - cp.tile * kDecodeTile - warp * kDecodeWarpTokens;
-            if (valid > 0) {
-                float s[2][4] = {};
+            uint32_t k_base = ring + stage * kGroupStage;
+            int valid = cp.len - cp.tile * G::kTile - group * kGroupTokens;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kGroupTokens && valid > 0; c0 += 16 * kM, valid -= 16 * kM, k_base += 16 * kM * G::kRowBytes) {
+                const uint32_t v_base = k_base + kGroupTokens * G::kRowBytes;
+                // All fragments of a block are loaded before its products, which run in two chains: what a warp waits for is
+                // latency, of the loads and from product to product.
+                float s[kM][4];
 #pragma unroll
-                for (int kk = 0; kk < kD / 16; ++kk) {
-                    uint32_t b[4];
-                    ldmatrix4(b, k_base + k_row * G::kRowBytes + (((2 * kk + k_half) ^ (k_row & 7)) << 4));
-                    mma16816<kBf16>(s[0], qf[kk], b[0], b[1]);
-                    mma16816<kBf16>(s[1], qf[kk], b[2], b[3]);
-                }
+                for (int i = 0; i < kM; ++i) {
+                    uint32_t a[kD / 16][4];
+                    const int row = 16 * i + k_row;
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                    for (int kk = 0; kk < kD / 16; ++kk) ldmatrix4(a[kk], k_base + row * G::kRowBytes + (((2 * kk + k_half) ^ (row & 7)) << 4));
+                    float even[4] = {}, odd[4] = {};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int token = n * 8 + 2 * (lane & 3) + (i & 1);
-                        s[n][i] = token < valid ? s[n][i] * p.scale_log2 : -INFINITY;
+                    for (int kk = 0; kk < kD / 16; kk += 2) {
+                        mma16816<kBf16>(even, a[kk], qf[kk][0], qf[kk][1]);
+                        mma16816<kBf16>(odd, a[kk + 1], qf[kk + 1][0], qf[kk + 1][1]);
                     }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) s[i][c] = (even[c] + odd[c]) * p.scale_log2;
+                }
+                if (valid < 16 * kM) {
+#pragma unroll
+                    for (int i = 0; i < kM; ++i)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (16 * i + (lane >> 2) + 8 * (c >> 1) >= valid) s[i][c] = -INFINITY;
+                }
                 float top[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float t = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-                    top[r] = fmaxf(m[r], t);
+                for (int c = 0; c < 2; ++c) {
+                    top[c] = fmaxf(s[0][c], s[0][c + 2]);
+                    if (kM == 2) top[c] = fmaxf(top[c], fmaxf(s[kM - 1][c], s[kM - 1][c + 2]));
                 }
-                if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
-                    const float f0 = top[0] > m[0] ? ptx::ex2(m[0] - top[0]) : 1.f, f1 = top[1] > m[1] ? ptx::ex2(m[1] - top[1]) : 1.f;
-                    m[0] = top[0];
-                    m[1] = top[1];
-                    l[0] *= f0;
-                    l[1] *= f1;
+                // (Always, where the reference is -infinity and the score is not.)
+                if (__any_sync(0xffffffffu, top[0] > ref[0] + kDecodeSlack || top[1] > ref[1] + kDecodeSlack)) {
 #pragma unroll
-                    for (int j = 0; j < kD / 8; ++j) { acc[j][0] *= f0; acc[j][1] *= f0; acc[j][2] *= f1; acc[j][3] *= f1; }
+                    for (int c = 0; c < 2; ++c) {
+                        float t = top[c];
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                        t = fmaxf(t, ref[c]);
+                        const float f = t > ref[c] ? ptx::ex2(ref[c] - t) : 1.f;
+                        ref[c] = t;
+                        l[c] *= f;
+#pragma unroll
+                        for (int j = 0; j < kD / 16; ++j) { acc[j][c] *= f; acc[j][c + 2] *= f; }
+                    }
                 }
-                // A row whose scores are all -infinity so far has no reference: its probabilities are 0.
-                const float ref0 = m[0] == -INFINITY ? 0.f : m[0] - kBias, ref1 = m[1] == -INFINITY ? 0.f : m[1] - kBias;
-                uint32_t hi[4], lo[4];
+                // A head whose scores are all -infinity so far has no reference: its probabilities are 0.
+                const float r0 = ref[0] == -INFINITY ? 0.f : ref[0] - kBias, r1 = ref[1] == -INFINITY ? 0.f : ref[1] - kBias;
+                uint32_t hi[kM][2], lo[kM][2];              // P^T as the B operand: tokens x heads
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int i = 0; i < kM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float p0 = ptx::ex2(s[n][2 * r] - (r ? ref1 : ref0)), p1 = ptx::ex2(s[n][2 * r + 1] - (r ? ref1 : ref0));
-                        l[r] += p0 + p1;
-                        const uint32_t h = ptx::pack2<kBf16>(p0, p1);
-                        float h0, h1;
-                        unpack2<kBf16>(h, h0, h1);
-                        hi[2 * n + r] = h;
-                        lo[2 * n + r] = ptx::pack2<kBf16>(p0 - h0, p1 - h1);
+                    for (int h = 0; h < 2; ++h) {
+                        const float p0 = ptx::ex2(s[i][2 * h] - r0), p1 = ptx::ex2(s[i][2 * h + 1] - r1);
+                        l[0] += p0;
+                        l[1] += p1;
+                        const uint32_t u = ptx::pack2<kBf16>(p0, p1);
+                        float u0, u1;
+                        unpack2<kBf16>(u, u0, u1);
+                        hi[i][h] = transpose8x8(u);
+                        lo[i][h] = transpose8x8(ptx::pack2<kBf16>(p0 - u0, p1 - u1));
                     }
 #pragma unroll
-                for (int j = 0; j < kD / 16; ++j) {
-                    uint32_t b[4];
-                    ldmatrix4_trans(b, v_base + v_row * G::kRowBytes + (((2 * j + v_half) ^ (v_row & 7)) << 4));
-                    mma16816<kBf16>(acc[2 * j], hi, b[0], b[1]);
-                    mma16816<kBf16>(acc[2 * j + 1], hi, b[2], b[3]);
-                    mma16816<kBf16>(acc[2 * j], lo, b[0], b[1]);
-                    mma16816<kBf16>(acc[2 * j + 1], lo, b[2], b[3]);
+                for (int i = 0; i < kM; ++i) {
+                    uint32_t a[kD / 16][4];
+                    const int row = 16 * i + v_row;
+#pragma unroll
+                    for (int j = 0; j < kD / 16; ++j) ldmatrix4_trans(a[j], v_base + row * G::kRowBytes + (((2 * j + v_half) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int j = 0; j < kD / 16; ++j) mma16816<kBf16>(acc[j], a[j], hi[i][0], hi[i][1]);
+#pragma unroll
+                    for (int j = 0; j < kD / 16; ++j) mma16816<kBf16>(acc[j], a[j], lo[i][0], lo[i][1]);
                 }
             }
             const bool ends = cp.tile == cp.n - 1;
             if (ends || left == 1) {
-                // ---- the four warps' sums meet in shared memory, each in the stage that its warp has just emptied
-                const int r0 = lane >> 2;
-                __syncwarp();
-                float* mine_o = reinterpret_cast<float*>(decode_smem + (size_t)(warp * kStages + stage) * G::kStageBytes);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-                    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-                    const int row = r0 + 8 * r;
-                    if ((lane & 3) == 0) warp_ml[warp][row] = make_float2(m[r], l[r]);
-#pragma unroll
-                    for (int j = 0; j < kD / 8; ++j) {
-                        const int piece = 2 * j + ((lane & 3) >> 1);     // 16-byte piece of the fp32 row, moved against bank conflicts
-                        *reinterpret_cast<float2*>(mine_o + row * kD + ((piece ^ (row & 7)) << 2) + ((lane & 1) << 1)) = make_float2(acc[j][2 * r], acc[j][2 * r + 1]);
-                    }
-                }
-                __syncthreads();
-                const int kvh = cp.block / p.head_blocks, first = (cp.block % p.head_blocks) * kDecodeRows;
-                const int rows = min(kDecodeRows, p.group - first);
+                // ---- the groups' sums meet in shared memory, each warp's in a part of the stage that its group has just emptied:
+                // [head][dimension], the dimension moved by 8 per pair of heads against bank conflicts
                 const bool starts = first_tile == 0, whole = starts && ends;
                 const int part = 2 * cta + (starts ? 1 : 0);
+                const int kvh = cp.block / p.head_blocks, first = (cp.block % p.head_blocks) * kRows;
+                const int rows = min(kRows, p.group - first);
+                const DecodeCursor<G::kTile> done = cp;
+                if (left > 1) {      // the next result's queries are on their way meanwhile
+                    cp.advance(p, blocks);
+                    first_tile = 0;
+                    load_q();
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
+                    if (lane < 4) warp_ml[warp][2 * lane + c] = make_float2(ref[c], l[c]);
+                }
+                group_sync();
+                constexpr int kOut = 8 * kD * 4;
+                float* mine_o = reinterpret_cast<float*>(ring_p + stage * kGroupStage + member * kOut);
+#pragma unroll
+                for (int j = 0; j < kD / 16; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        mine_o[(2 * (lane & 3) + (c & 1)) * kD + ((16 * j + (lane >> 2) + 8 * (c >> 1)) ^ ((lane & 3) << 3))] = acc[j][c];
+                __syncthreads();
                 for (int i = tid; i < rows * (kD / 4); i += kDecodeThreads) {
-                    const int row = i / (kD / 4), piece = i % (kD / 4);
+                    const int row = i / (kD / 4), piece = i % (kD / 4), m = row >> 3, r = row & 7;
                     float big = -INFINITY;
 #pragma unroll
-                    for (int w = 0; w < kDecodeWarps; ++w) big = fmaxf(big, warp_ml[w][row].x);
+                    for (int g = 0; g < kGroups; ++g) big = fmaxf(big, warp_ml[g * kN + m][r].x);
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                     float total_l = 0.f;
 #pragma unroll
-                    for (int w = 0; w < kDecodeWarps; ++w) {
-                        const float2 ml = warp_ml[w][row];
+                    for (int g = 0; g < kGroups; ++g) {
+                        const float2 ml = warp_ml[g * kN + m][r];
                         // A warp without a finite score has sums of 0 (or NaN, which is to stay): its weight is 1.
                         const float f = ml.x == -INFINITY ? 1.f : ptx::ex2(ml.x - big);
-                        const float* from = reinterpret_cast<const float*>(decode_smem + (size_t)(w * kStages + stage) * G::kStageBytes);
-                        const float4 x = *reinterpret_cast<const float4*>(from + row * kD + ((piece ^ (row & 7)) << 2));
+                        const float* from = reinterpret_cast<const float*>(decode_smem + (size_t)(g * kStages + stage) * kGroupStage + m * kOut);
+                        const float4 x = *reinterpret_cast<const float4*>(from + r * kD + ((4 * piece) ^ ((r >> 1) << 3)));
                         sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
                         total_l += f * ml.y;
                     }
                     const int head = kvh * p.group + first + row;
                     if (whole) {
                         const float inv = 1.f / total_l;
-                        *reinterpret_cast<uint2*>(p.o + (long long)cp.b * p.o_request + (long long)head * p.o_head + 4 * piece) =
+                        *reinterpret_cast<uint2*>(p.o + (long long)done.b * p.o_request + (long long)head * p.o_head + 4 * piece) =
                             make_uint2(ptx::pack2<kBf16>(sum.x * inv, sum.y * inv), ptx::pack2<kBf16>(sum.z * inv, sum.w * inv));
-                        if (p.lse && piece == 0) p.lse[(long long)cp.b * p.H + head] = (big - kBias + log2f(total_l)) * 0.6931471805599453f;
+                        if (p.lse && piece == 0) p.lse[(long long)done.b * p.H + head] = (big - kBias + log2f(total_l)) * 0.6931471805599453f;
                     } else {
-                        *reinterpret_cast<float4*>(p.part_o + ((size_t)part * kDecodeRows + row) * kD + 4 * piece) = sum;
-                        if (piece == 0) p.part_ml[(size_t)part * kDecodeRows + row] = make_float2(big, total_l);
+                        *reinterpret_cast<float4*>(p.part_o + ((size_t)part * kRows + row) * kD + 4 * piece) = sum;
+                        if (piece == 0) p.part_ml[(size_t)part * kRows + row] = make_float2(big, total_l);
                     }
                 }
-                if (starts && !ends) {
-                    // Cut by the end of this share: the join of the parts is this CTA's to describe.
-                    const uint64_t last = begin + (uint64_t)(decode_share_begin(total, ctas, cta + 1) - begin) - 1 + (uint64_t)(cp.n - 1 - cp.tile);
-                    join = make_int4(decode_cta_of(total, ctas, last) - cta + 1, cp.b, cp.block, 0);
-                }
                 __syncthreads();   // the stages may be filled again
-                m[0] = m[1] = -INFINITY;
-                l[0] = l[1] = 0.f;
-#pragma unroll
-                for (int j = 0; j < kD / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-                if (left > 1) {
-                    cp.advance(p, blocks);
-                    first_tile = 0;
-                    load_q();
+                if (!whole && tid == 0) {
+                    // Which CTAs hold the parts: those of the result's first and last tile.
+                    const uint64_t now = end - (uint64_t)left;                   // this tile's place in the line
+                    const int c0 = decode_cta_of(total, ctas, now - (uint64_t)done.tile), c1 = decode_cta_of(total, ctas, now + (uint64_t)(done.n - 1 - done.tile));
+                    p.join[part] = make_int4(c1 - c0 + 1, c0, done.b, done.block);
                 }
+                joins |= whole ? 0 : 1 << (part & 1);
+                clear();
             } else {
                 ++cp.tile;
             }
@@ -365,10 +438,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_paged_kernel(const D
         }
         cp_async_wait<0>();
     }
-    if (tid == 0) p.join[cta] = join;
+    if (tid == 0) {
+        if (!(joins & 1)) p.join[2 * cta] = make_int4(0, 0, 0, 0);
+        if (!(joins & 2)) p.join[2 * cta + 1] = make_int4(0, 0, 0, 0);
+    }
     // ---- requests without tokens
     for (int b = cta; b < p.B; b += gridDim.x) {
-        if (decode_len(p, b) != 0) continue;
+        if (decode_cut(p, p.seq_len[b]) != 0) continue;
         for (int i = tid; i < p.H * (kD / 8); i += kDecodeThreads)
             *reinterpret_cast<uint4*>(p.o + (long long)b * p.o_request + (long long)(i / (kD / 8)) * p.o_head + (i % (kD / 8)) * 8) = make_uint4(0, 0, 0, 0);
         if (p.lse)
@@ -376,57 +452,104 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_paged_kernel(const D
     }
 }
 
-// Joins the parts of the request that CTA blockIdx.x began and did not finish, row blockIdx.y of its 16: o = sum_i f_i o_i / sum_i f_i l_i,
-// f_i = 2^(m_i - max m).  The eight warps take the parts in turn, each over all columns; their sums are added in a fixed order.
+// Joins cut results: o = sum_i f_i o_i / sum_i f_i l_i over their parts, f_i = 2^(m_i - max m).  The n CTAs that hold the parts of a result
+// share its rows, so that a result cut into many parts has many hands.  A CTA has rows of at most two results; its eight warps take
+// one each, or where there are fewer than eight rows, as many to a row as there are, which take the parts in turn and
+// add up in a fixed order.
 constexpr int kJoinThreads = 256;
 template <int kD, int kBf16>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeParams p)
 {
     constexpr int kWarps = kJoinThreads / 32, kCols = kD / 32;     // columns a lane sums
-    constexpr float kBias = kBf16 ? 0.f : 15.f;
+    constexpr float kBias = kBf16 ? 0.f : 7.f;
     __shared__ float sums[kWarps][kD];
-    __shared__ float sums_l[kWarps];
+    __shared__ float2 sums_ml[kWarps];
+    const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, block_rows = decode_rows(p.group);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int4 join = p.join[blockIdx.x];
-    if (join.x == 0) return;
-    const int n = join.x, row = blockIdx.y, c0 = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int kvh = join.z / p.head_blocks, first = (join.z % p.head_blocks) * kDecodeRows;
-    if (first + row >= p.group) return;
-    auto entry = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * kDecodeRows + row; };
-    float big = -INFINITY;
-    for (int i = lane; i < n; i += 32) big = fmaxf(big, p.part_ml[entry(i)].x);
+    const int4 joins[2] = {p.join[2 * cta], p.join[2 * cta + 1]};
+    // Of a result with n parts from CTA c0 on, this CTA takes rows cta - c0, cta - c0 + n, ...
+    auto rows_of = [&](const int4& j) { return min(block_rows, p.group - (j.w % p.head_blocks) * block_rows); };
+    auto my_rows = [&](const int4& j) {
+        const int turn = cta - j.y, rows = j.x > 0 ? rows_of(j) : 0;
+        return turn < rows ? (rows - turn + j.x - 1) / j.x : 0;
+    };
+    const int rows0 = my_rows(joins[0]), items = rows0 + my_rows(joins[1]);
+    const int to_a_row = items > 4 ? 1 : items > 2 ? 2 : items > 1 ? 4 : 8;     // warps
+    const int at_once = kWarps / to_a_row, lot = warp % to_a_row;
+    for (int r0 = 0; r0 < items; r0 += at_once) {
+        const int item = r0 + warp / to_a_row;
+        const bool there = item < items;
+        const int4 join = item < rows0 ? joins[0] : joins[1];
+        const int n = there ? join.x : 0, c0 = join.y, row = cta - c0 + (item < rows0 ? item : item - rows0) * n;
+        auto entry = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * block_rows + row; };
+        // Running reference, sum and columns over this warp's parts, kAhead of them read at a time.
+        constexpr int kAhead = 4;
+        float big = -INFINITY, acc[kCols] = {}, l = 0.f;
+        for (int i0 = lot; i0 < n; i0 += kAhead * to_a_row) {
+            float2 ml[kAhead];
+            float x[kAhead][kCols];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-    float acc[kCols] = {}, l = 0.f;
-#pragma unroll 4
-    for (int i = warp; i < n; i += kWarps) {
-        const float2 ml = p.part_ml[entry(i)];
-        const float f = ml.x == -INFINITY ? 1.f : ptx::ex2(ml.x - big);
-        const float* from = p.part_o + entry(i) * kD + lane * kCols;
-        float x[kCols];
-        if (kCols == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(from);
-            x[0] = v.x; x[1] = v.y; x[kCols - 2] = v.z; x[kCols - 1] = v.w;
-        } else {
-            const float2 v = *reinterpret_cast<const float2*>(from);
-            x[0] = v.x; x[1] = v.y;
+            for (int a = 0; a < kAhead; ++a) {
+                const int i = i0 + a * to_a_row;
+                ml[a] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) x[a][c] = 0.f;
+                if (i < n) {
+                    ml[a] = p.part_ml[entry(i)];
+                    const float* from = p.part_o + entry(i) * kD + lane * kCols;
+                    if (kCols == 4) {
+                        const float4 v = *reinterpret_cast<const float4*>(from);
+                        x[a][0] = v.x; x[a][1] = v.y; x[a][kCols - 2] = v.z; x[a][kCols - 1] = v.w;
+                    } else {
+                        const float2 v = *reinterpret_cast<const float2*>(from);
+                        x[a][0] = v.x; x[a][1] = v.y;
+                    }
+                }
+            }
+            float top = big;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) top = fmaxf(top, ml[a].x);
+            const float keep = big == -INFINITY ? 1.f : ptx::ex2(big - top);     // (parts without a finite score have sums of 0 or NaN)
+            big = top;
+            l *= keep;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) acc[c] *= keep;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const float f = ml[a].x == -INFINITY ? 1.f : ptx::ex2(ml[a].x - top);
+                l += f * ml[a].y;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) acc[c] += f * x[a][c];
+            }
         }
+        if (to_a_row > 1) {
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) acc[c] += f * x[c];
-        l += f * ml.y;
-    }
+            for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = acc[c];
+            if (lane == 0) sums_ml[warp] = make_float2(big, l);
+            __syncthreads();
+            if (lot == 0) {
+                for (int w = 0; w < to_a_row; ++w) big = fmaxf(big, sums_ml[warp + w].x);
+                l = 0.f;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = acc[c];
-    if (lane == 0) sums_l[warp] = l;
-    __syncthreads();
-    if (threadIdx.x < kD / 2) {
-        float a = 0.f, b = 0.f, t = 0.f;
+                for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
+                for (int w = 0; w < to_a_row; ++w) {
+                    const float2 ml = sums_ml[warp + w];
+                    const float f = ml.x == -INFINITY ? 1.f : ptx::ex2(ml.x - big);
+                    l += f * ml.y;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) { a += sums[w][2 * threadIdx.x]; b += sums[w][2 * threadIdx.x + 1]; t += sums_l[w]; }
-        const float inv = 1.f / t;
-        const int head = kvh * p.group + first + row;
-        *reinterpret_cast<uint32_t*>(p.o + (long long)join.y * p.o_request + (long long)head * p.o_head + 2 * threadIdx.x) = ptx::pack2<kBf16>(a * inv, b * inv);
-        if (p.lse && threadIdx.x == 0) p.lse[(long long)join.y * p.H + head] = (big - kBias + log2f(t)) * 0.6931471805599453f;
+                    for (int c = 0; c < kCols; ++c) acc[c] += f * sums[warp + w][lane * kCols + c];
+                }
+            }
+            __syncthreads();
+        }
+        if (there && lot == 0) {
+            const float inv = 1.f / l;
+            const int head = (join.w / p.head_blocks) * p.group + (join.w % p.head_blocks) * block_rows + row;
+            uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (long long)join.z * p.o_request + (long long)head * p.o_head + lane * kCols);
+#pragma unroll
+            for (int c = 0; c < kCols / 2; ++c) out[c] = ptx::pack2<kBf16>(acc[2 * c] * inv, acc[2 * c + 1] * inv);
+            if (p.lse && lane == 0) p.lse[(long long)join.z * p.H + head] = (big - kBias + log2f(l)) * 0.6931471805599453f;
+        }
     }
 }
 

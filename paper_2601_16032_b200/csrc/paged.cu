@@ -210,19 +210,23 @@ RopeKernel rope_kernel(int d, int dtype, int style, bool backward) {
 }
 
 using DecodeKernel = void (*)(const DecodeParams);
+template <int kD, int kBf16, int kN>
+int launch_decode_rows(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
+    constexpr int kSmem = DecodeGeometry<kD>::kSmem, kBit = kRaisedDecode + ((kD == 128) * 2 + kBf16) * 3 + kN / 2;
+    DecodeKernel kernel = decode_paged_kernel<kD, kBf16, kN>;
+    int rc = raise_smem(dev, ds, (const void*)kernel, kBit, kSmem);
+    return rc ? rc : launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, 0, false, p));
+}
 template <int kD, int kBf16>
 int launch_decode(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
-    constexpr int kSmem = DecodeGeometry<kD>::kSmem;
-    DecodeKernel kernel = decode_paged_kernel<kD, kBf16>;
-    int rc = raise_smem(dev, ds, (const void*)kernel, kRaisedDecode + (kD == 128) * 2 + kBf16, kSmem);
-    if (rc) return rc;
-    if ((rc = launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, 0, false, p)))) return rc;
-    const int rows = p.group < kDecodeRows ? p.group : kDecodeRows;
-    return launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, rows, kJoinThreads, 0, st, 0, true, p));
+    const int rows = decode_rows(p.group);
+    int rc = rows == 8 ? launch_decode_rows<kD, kBf16, 1>(dev, ds, p, grid, st) : rows == 16 ? launch_decode_rows<kD, kBf16, 2>(dev, ds, p, grid, st)
+                                                                                : launch_decode_rows<kD, kBf16, 4>(dev, ds, p, grid, st);
+    return rc ? rc : launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, 1, kJoinThreads, 0, st, 0, true, p));
 }
 
-size_t decode_workspace(int grid, int d) {
-    return (size_t)grid * (sizeof(int4) + 2 * kDecodeRows * (sizeof(float2) + sizeof(float) * (size_t)d));
+size_t decode_workspace(int grid, int rows, int d) {
+    return (size_t)grid * 2 * (sizeof(int4) + (size_t)rows * (sizeof(float2) + sizeof(float) * (size_t)d));
 }
 
 int check_decode_shape(int B, int H, int kv_heads, int d, const attn_decode_opts& z) {
@@ -236,7 +240,7 @@ int check_decode_shape(int B, int H, int kv_heads, int d, const attn_decode_opts
     return ATTN_OK;
 }
 int decode_grid(int sm_count, const attn_decode_opts& z) {
-    const int most = 2 * sm_count;   // two CTAs of 96 KiB an SM
+    const int most = 3 * sm_count;   // three CTAs of 64 KiB an SM
     return z.max_ctas > 0 && z.max_ctas < most ? z.max_ctas : most;
 }
 
@@ -405,10 +409,11 @@ int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_
     out->grid = decode_grid(sm_count, z);
     out->threads = kDecodeThreads;
     out->smem_bytes = d == 128 ? DecodeGeometry<128>::kSmem : DecodeGeometry<64>::kSmem;
-    out->tile_tokens = kDecodeTile;
-    out->head_blocks = (H / kv_heads + kDecodeRows - 1) / kDecodeRows;
+    out->tile_tokens = decode_tile(d);
+    const int rows = decode_rows(H / kv_heads);
+    out->head_blocks = (H / kv_heads + rows - 1) / rows;
     out->min_tiles = kDecodeMinTiles;
-    out->workspace_bytes = decode_workspace(out->grid, d);
+    out->workspace_bytes = decode_workspace(out->grid, rows, d);
     return ATTN_OK;
 }
 
@@ -423,7 +428,7 @@ int attn_decode_trace(const int* seq_len, int B, int H, int kv_heads, int d, con
     uint64_t total = 0;
     for (int b = 0; b < B; ++b) {
         if (seq_len[b] < 0) return fail(ATTN_ERR_INVALID_ARG, "a length is negative");
-        total += (uint64_t)decode_tiles(seq_len[b]) * blocks;
+        total += (uint64_t)decode_tiles(seq_len[b], plan.tile_tokens) * blocks;
     }
     *n = 0;
     if (total == 0) return ATTN_OK;
@@ -432,7 +437,7 @@ int attn_decode_trace(const int* seq_len, int B, int H, int kv_heads, int d, con
     uint64_t first = 0;     // the line's tiles before request b, block k
     int cta = 0;
     for (int b = 0; b < B; ++b) {
-        const int tiles = decode_tiles(seq_len[b]);
+        const int tiles = decode_tiles(seq_len[b], plan.tile_tokens);
         for (int k = 0; tiles > 0 && k < blocks; ++k, first += tiles) {
             for (int t = 0; t < tiles;) {
                 while (decode_share_begin(total, ctas, cta + 1) <= first + t) ++cta;
@@ -482,8 +487,10 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     int dev = 0;
     if ((rc = current_device(&ds, &dev))) return rc;
     const int grid = decode_grid(ds.sm_count, z);
-    if (workspace_bytes < decode_workspace(grid, c.d)) return fail(ATTN_ERR_INVALID_ARG, "the workspace needs %zu bytes", decode_workspace(grid, c.d));
-    const Region ws = {workspace, 1, 0, 1, 0, (long long)decode_workspace(grid, c.d)};
+    const int rows = decode_rows(H / c.kv_heads);
+    const size_t need = decode_workspace(grid, rows, c.d);
+    if (workspace_bytes < need) return fail(ATTN_ERR_INVALID_ARG, "the workspace needs %zu bytes", need);
+    const Region ws = {workspace, 1, 0, 1, 0, (long long)need};
     const Region lse = {z.lse, 1, 0, 1, 0, (long long)B * H * 4};
     const Region lens = {seq_len, 1, 0, 1, 0, (long long)B * 4}, table = {block_table, 1, 0, 1, 0, ((long long)(B - 1) * table_stride + max_pages) * 4};
     const Region ins[] = {rq, span_of(c, c.k), span_of(c, c.v), lens, table};
@@ -506,14 +513,14 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     p.seq_len = seq_len;
     p.status = ds.status;
     p.join = static_cast<int4*>(workspace);
-    p.part_ml = reinterpret_cast<float2*>(p.join + grid);
-    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * grid * kDecodeRows);
+    p.part_ml = reinterpret_cast<float2*>(p.join + 2 * grid);
+    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * grid * rows);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.B = B;
     p.H = H;
     p.kv_heads = c.kv_heads;
     p.group = H / c.kv_heads;
-    p.head_blocks = (p.group + kDecodeRows - 1) / kDecodeRows;
+    p.head_blocks = (p.group + rows - 1) / rows;
     const long long most = (long long)max_pages * c.page_size;
     p.max_len = most < 2147483647ll ? (int)most : 2147483647;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -19,8 +19,8 @@ def check(lengths, H, kv_heads, d, max_ctas=0, sm_count=148):
     o.max_ctas = max_ctas
     plan = sa.attn_decode_query_plan(len(lengths), H, kv_heads, d, o, sm_count)
     group = H // kv_heads
-    assert plan.head_blocks == -(-group // 16) and plan.grid <= (max_ctas or 2 * sm_count)
-    assert plan.workspace_bytes >= plan.grid * 2 * 16 * (d + 2) * 4
+    assert plan.head_blocks == -(-group // 32) and plan.grid <= (max_ctas or 3 * sm_count)
+    assert plan.workspace_bytes >= plan.grid * 2 * min(group, 32) * (d + 2) * 4
     trace = sa.attn_decode_trace(lengths, H, kv_heads, d, o, sm_count)
     tiles = [-(-n // plan.tile_tokens) for n in lengths]
     total = sum(tiles) * kv_heads * plan.head_blocks
