@@ -198,6 +198,19 @@ void fill_rope(RopeParams* p, int T, int H, int kv_heads, const void* q_weight, 
     p->weight_f32 = z.weight_f32;
 }
 
+void rope_groups(RopeParams* p, int d, bool cached) {
+    const int rows = 32 / (d / 8);
+    p->q_groups = (p->H + rows - 1) / rows;
+    p->k_groups = (p->kv_heads + rows - 1) / rows;
+    p->groups = p->q_groups + (cached ? 2 : 1) * p->k_groups;
+}
+// As many CTAs as are resident at a time, or as give every warp kRopeMinGroups row groups.
+int rope_grid(const RopeParams& p, int most) {
+    constexpr int kRopeMinGroups = 2;
+    const long long each = (long long)kRopeWarps * kRopeMinGroups, need = ((long long)p.T * p.groups + each - 1) / each;
+    return need < 1 ? 1 : need < most ? (int)need : most;
+}
+
 using RopeKernel = void (*)(const RopeParams);
 template <int kD, int kBf16>
 RopeKernel rope_kernel_of(int style, bool backward) {
@@ -313,7 +326,6 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, 
         (rc = rows_of("q_out", q_out, z.q_out_token, z.q_out_head, T, H, d, true, &rqo)))
         return rc;
     if (k_out && (rc = rows_of("k_out", k_out, z.k_out_token, z.k_out_head, T, kv_heads, d, true, &rko))) return rc;
-    p.rows = FastDiv((uint32_t)(H + kv_heads));
     if (z.cache) {
         if ((rc = rows_of("v", v, z.v_token, z.v_head, T, kv_heads, d, false, &rv))) return rc;
         attn_kv_cache c;
@@ -325,7 +337,6 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, 
                 return fail(ATTN_ERR_INVALID_ARG, "the cache must not overlap the call's other arrays");
         p.cache = view_of(c);
         p.slot = z.slot;
-        p.rows = FastDiv((uint32_t)(H + 2 * kv_heads));
     }
     if ((overlap(rqo, rq) && !same(rqo, rq)) || overlap(rqo, rk) || overlap(rqo, rv) || overlap(rqo, rko) || (overlap(rko, rk) && !same(rko, rk)) ||
         overlap(rko, rq) || overlap(rko, rv))
@@ -337,8 +348,8 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, 
     p.q = in_of(rq); p.k = in_of(rk); p.q_out = out_of(rqo);
     if (k_out) p.k_out = out_of(rko);
     if (z.cache) p.v = in_of(rv);
-    p.tokens_per_cta = T <= 4 * ds.sm_count ? 1 : 2;
-    const int grid = (T + p.tokens_per_cta - 1) / p.tokens_per_cta;
+    rope_groups(&p, d, z.cache != nullptr);
+    const int grid = rope_grid(p, kRopeForwardCtas * ds.sm_count);
     rope_kernel(d, dtype, rot_style, false)<<<grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
     if ((rc = launch_status(cudaGetLastError()))) return rc;
     return z.check_mode ? read_status(nullptr) : ATTN_OK;
@@ -378,12 +389,9 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
     if ((rc = current_device(&ds, nullptr))) return rc;
     fill_rope(&p, T, H, kv_heads, q_weight, k_weight, eps, position, inv_freq, rot_dim, z, ds);
     p.q = in_of(rq); p.k = in_of(rk); p.dq_out = in_of(rgq); p.dk_out = in_of(rgk); p.q_out = out_of(rdq); p.k_out = out_of(rdk);
-    p.rows = FastDiv((uint32_t)(H + kv_heads));
     p.partial = static_cast<float*>(workspace);
-    p.tokens_per_cta = T <= 4 * ds.sm_count ? 1 : 2;
-    const int chunks = (T + p.tokens_per_cta - 1) / p.tokens_per_cta;
-    int grid = 4 * ds.sm_count < kRopeMaxCtas ? 4 * ds.sm_count : kRopeMaxCtas;
-    if (grid > chunks) grid = chunks > 0 ? chunks : 1;
+    rope_groups(&p, d, false);
+    const int grid = rope_grid(p, kRopeBackwardCtas * ds.sm_count < kRopeMaxCtas ? kRopeBackwardCtas * ds.sm_count : kRopeMaxCtas);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     rope_kernel(d, dtype, rot_style, true)<<<grid, kRopeThreads, 0, st>>>(p);
     if ((rc = launch_status(cudaGetLastError()))) return rc;

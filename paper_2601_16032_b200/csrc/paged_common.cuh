@@ -36,6 +36,14 @@ struct CacheView {
 
 __device__ __forceinline__ void note_index(int* status, int code) { atomicCAS(status, 0, code); }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes)   // copies `bytes` (16 or 0), zero-fills the rest
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
 template <int kBf16>
 __device__ __forceinline__ void unpack2(uint32_t u, float& lo, float& hi) {
     if (kBf16) {
@@ -44,18 +52,6 @@ __device__ __forceinline__ void unpack2(uint32_t u, float& lo, float& hi) {
     } else {
         asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(u));
     }
-}
-
-template <int kBf16>
-__device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
-    unpack2<kBf16>(u.x, x[0], x[1]);
-    unpack2<kBf16>(u.y, x[2], x[3]);
-    unpack2<kBf16>(u.z, x[4], x[5]);
-    unpack2<kBf16>(u.w, x[6], x[7]);
-}
-template <int kBf16>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return make_uint4(ptx::pack2<kBf16>(x[0], x[1]), ptx::pack2<kBf16>(x[2], x[3]), ptx::pack2<kBf16>(x[4], x[5]), ptx::pack2<kBf16>(x[6], x[7]));
 }
 
 }  // namespace sawtooth

@@ -1,12 +1,15 @@
 // RMS norm of every query and key head with the position rotation, the append to the paged cache, and the gradients.
 //
-// All of it is one pass over memory (per row of d values some 100 instructions against 4 d bytes), so the kernels are laid
-// out for wide loads in flight: a row is held by kD / 8 lanes with 16 bytes each; its sum of squares is reduced by
-// shuffles; the partner of a rotated pair is in the same lane (adjacent pairs) or rot_dim / 16 lanes away (halves).
-// A token's angles are the same for all of its heads: a CTA takes a few tokens, computes their sines and cosines once into shared
-// memory while the first rows are on their way, and then walks the tokens' rows.  Angles are formed and reduced to a part of a
-// turn in 64 bits (position * inv_freq loses its fraction in 32 bits when positions are far); the sine and cosine of the part, and
-// everything else, are 32-bit.
+// All of it is one pass over memory, 4 d bytes a row (6 d backward), and an SM has some 60 warp instructions to spend on 512 bytes,
+// so it is the instructions that decide whether memory is kept busy.  A row is held by kD / 8 lanes, four rotated pairs each: with
+// halves as pairs a lane takes four columns from each half (two 8-byte loads), so that no lane needs another's columns; a
+// warp works on 32 / (kD / 8) rows of one token at a time.  Weight and rotation together are linear in the pair (u, v) and the same for all
+// heads of a token:
+//     u' = r (u wu cos - v wv sin),   v' = r (v wv cos + u wu sin),   r = 1 / sqrt(mean x^2 + eps),
+// so a lane keeps the four products of its pairs in registers from head to head, and the arithmetic runs in packed pairs of
+// fp32.  The row groups of all tokens are one line that the warps of a resident grid share out evenly; a warp computes a token's sines and
+// cosines when it gets there.  Angles are formed and reduced to a part of a turn in 64 bits (position * inv_freq loses its fraction in
+// 32 bits when positions are far); the sine and cosine of the part, and everything else, are 32-bit.
 #pragma once
 #include "paged_common.cuh"
 
@@ -22,7 +25,8 @@ struct RopeOut {
 };
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 4;    // tokens a CTA takes at a time
+constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeForwardCtas = 3, kRopeBackwardCtas = 2, kRopeBackwardDepth = 4;   // CTAs of an SM, row groups asked for ahead
 
 struct RopeParams {
     RopeTensor q, k, v;          // the projections
@@ -37,62 +41,105 @@ struct RopeParams {
     float* partial;              // backward pass: [CTA][2][d] sums for the weights
     int* status;
     float eps;
-    int T, H, kv_heads, rot, weight_f32, tokens_per_cta;
-    FastDiv rows;                // rows.d = rows of a token: H + kv_heads, or with a cache H + 2 kv_heads
+    int T, H, kv_heads, rot, weight_f32;
+    int q_groups, k_groups;      // row groups of a token's queries, and of its keys (as many again of values with a cache)
+    int groups;                  // of a token in all
 };
 
-template <int kD>
-struct RopeShared {
-    float cosine[kRopeMaxTokens][kD / 2];
-    float sine[kRopeMaxTokens][kD / 2];
-    long long cache_at[kRopeMaxTokens];   // element offset of the token's first cache row; -1: none, -2: leave the token alone
-};
-
-// Angles of tokens t0 .. t0 + n - 1 into shared memory, and where their cache rows are.
-template <int kD>
-__device__ __forceinline__ void rope_prepare(const RopeParams& p, RopeShared<kD>& s, int t0, int n, bool backward)
+// The row groups [begin, end) of the line that this warp takes.
+__device__ __forceinline__ void rope_share(const RopeParams& p, long long& begin, long long& end)
 {
-    const int half = p.rot >> 1;
-    for (int i = threadIdx.x; i < n * (kD / 2); i += kRopeThreads) {
-        const int t = i / (kD / 2), j = i % (kD / 2);
-        if (j >= half) continue;
-        const double turns = (double)p.position[t0 + t] * p.inv_freq[j] * 0.15915494309189535;   // / 2 pi
-        float sn, cs;
-        sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-        s.cosine[t][j] = cs;
-        s.sine[t][j] = backward ? -sn : sn;
-    }
-    if (!backward && threadIdx.x < n) {
-        long long at = -1;
-        if (p.slot) {
-            const long long slot = p.slot[t0 + threadIdx.x];
-            if (slot < 0) {
-                at = -2;
-            } else {
-                const long long page = slot < 2147483648ll ? (long long)p.cache.page.div((uint32_t)slot) : slot / p.cache.page.d;
-                if (page >= p.cache.num_pages) note_index(p.status, kIndexSlot);
-                else at = page * p.cache.page_stride + (slot - page * p.cache.page.d) * p.cache.token_stride;
-            }
+    const long long total = (long long)p.T * p.groups, warps = (long long)gridDim.x * kRopeWarps, me = (long long)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
+    const long long each = total / warps, more = total - each * warps;     // the first `more` warps take one more
+    begin = each * me + (me < more ? me : more);
+    end = begin + each + (me < more ? 1 : 0);
+}
+
+// Cosines and sines of a token's angles into this warp's shared memory.
+__device__ __forceinline__ void rope_angles(const RopeParams& p, int token, float2* turn)
+{
+    __syncwarp();
+    if (p.rot > 0) {
+        const double position = (double)p.position[token];
+        for (int i = threadIdx.x & 31; i < (p.rot >> 1); i += 32) {
+            const double turns = position * p.inv_freq[i] * 0.15915494309189535;   // / 2 pi
+            float sn, cs;
+            sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+            turn[i] = make_float2(cs, sn);
         }
-        s.cache_at[threadIdx.x] = at;
     }
+    __syncwarp();
 }
 
-__device__ __forceinline__ void load_weight(const void* w, int f32, int bf16, int e0, float (&out)[8])
+__device__ __forceinline__ float rope_weight(const void* w, int f32, int bf16, int e)
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = 1.f;
-    if (!w) return;
-    if (f32) {
-        const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(w) + e0);
-        const float4 a = f[0], b = f[1];
-        out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w; out[4] = b.x; out[5] = b.y; out[6] = b.z; out[7] = b.w;
-    } else {
-        const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + e0);
-        if (bf16) unpack8<1>(u, out); else unpack8<0>(u, out);
-    }
+    if (!w) return 1.f;
+    if (f32) return static_cast<const float*>(w)[e];
+    const uint32_t u = static_cast<const uint16_t*>(w)[e];
+    float lo, hi;
+    if (bf16) unpack2<1>(u, lo, hi); else unpack2<0>(u, lo, hi);
+    return lo;
 }
 
+// The eight columns of a lane as four pairs (u_i, v_i).  Halves: u_i from the first half of the rotated columns, v_i from the second, or
+// eight columns that do not turn; adjacent: neighbours.  Pair i of a lane that turns has the angle 4 * part + i.
+template <int kAdjacent>
+struct RopeColumns {
+    int c0, c1;      // first of four columns, and of four more
+    bool turns;
+    __device__ __forceinline__ RopeColumns(int rot, int part) {
+        turns = 8 * part < rot;
+        c0 = !kAdjacent && turns ? 4 * part : 8 * part;
+        c1 = !kAdjacent && turns ? (rot >> 1) + 4 * part : 8 * part + 4;
+    }
+    __device__ __forceinline__ int u(int i) const { return kAdjacent ? c0 + 2 * i : c0 + i; }
+    __device__ __forceinline__ int v(int i) const { return kAdjacent ? c0 + 2 * i + 1 : c1 + i; }
+    __device__ __forceinline__ uint4 load(const uint16_t* row) const {
+        if (kAdjacent) return *reinterpret_cast<const uint4*>(row + c0);
+        const uint2 a = *reinterpret_cast<const uint2*>(row + c0), b = *reinterpret_cast<const uint2*>(row + c1);
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    __device__ __forceinline__ void store(uint16_t* row, const uint4& x) const {
+        if (kAdjacent) {
+            *reinterpret_cast<uint4*>(row + c0) = x;
+        } else {
+            *reinterpret_cast<uint2*>(row + c0) = make_uint2(x.x, x.y);
+            *reinterpret_cast<uint2*>(row + c1) = make_uint2(x.z, x.w);
+        }
+    }
+};
+
+// A lane's raw columns as fp32 pairs: (u0, u1), (u2, u3) and (v0, v1), (v2, v3); and back, rounded.
+template <int kBf16, int kAdjacent>
+__device__ __forceinline__ void rope_unpack(const uint4& x, ptx::f32x2 (&u)[2], ptx::f32x2 (&v)[2])
+{
+    float l[4], h[4];
+    unpack2<kBf16>(x.x, l[0], h[0]);
+    unpack2<kBf16>(x.y, l[1], h[1]);
+    unpack2<kBf16>(x.z, l[2], h[2]);
+    unpack2<kBf16>(x.w, l[3], h[3]);
+    u[0] = kAdjacent ? ptx::pack_f32x2(l[0], l[1]) : ptx::pack_f32x2(l[0], h[0]);
+    u[1] = kAdjacent ? ptx::pack_f32x2(l[2], l[3]) : ptx::pack_f32x2(l[1], h[1]);
+    v[0] = kAdjacent ? ptx::pack_f32x2(h[0], h[1]) : ptx::pack_f32x2(l[2], h[2]);
+    v[1] = kAdjacent ? ptx::pack_f32x2(h[2], h[3]) : ptx::pack_f32x2(l[3], h[3]);
+}
+template <int kBf16, int kAdjacent>
+__device__ __forceinline__ uint4 rope_pack(const ptx::f32x2 (&u)[2], const ptx::f32x2 (&v)[2])
+{
+    float a[4], b[4];
+    ptx::unpack_f32x2(u[0], a[0], a[1]);
+    ptx::unpack_f32x2(u[1], a[2], a[3]);
+    ptx::unpack_f32x2(v[0], b[0], b[1]);
+    ptx::unpack_f32x2(v[1], b[2], b[3]);
+    if (kAdjacent) return make_uint4(ptx::pack2<kBf16>(a[0], b[0]), ptx::pack2<kBf16>(a[1], b[1]), ptx::pack2<kBf16>(a[2], b[2]), ptx::pack2<kBf16>(a[3], b[3]));
+    return make_uint4(ptx::pack2<kBf16>(a[0], a[1]), ptx::pack2<kBf16>(a[2], a[3]), ptx::pack2<kBf16>(b[0], b[1]), ptx::pack2<kBf16>(b[2], b[3]));
+}
+__device__ __forceinline__ float pair_sum(ptx::f32x2 x)
+{
+    float lo, hi;
+    ptx::unpack_f32x2(x, lo, hi);
+    return lo + hi;
+}
 template <int kLanes>
 __device__ __forceinline__ float row_sum(float x)
 {
@@ -101,202 +148,302 @@ __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
-// Rotates a row (this lane's eight values y, columns 8 * part ..) by the angles of cs / sn.  Whole warps.
-template <int kD, int kAdjacent>
-__device__ __forceinline__ void rotate_row(float (&y)[8], const float* cs, const float* sn, int rot, int part)
+// Rows reach a warp through a ring of its own in shared memory, filled kRopeDepth row groups ahead by 16-byte asynchronous copies, so that
+// what is in flight costs no registers.  RopeStream is the place that the copies have reached: kind by kind within a token.
+constexpr int kRopeDepth = 8;
+
+struct RopeSegment {        // row groups of one token and kind that this warp takes
+    int token, kind, first, rows_left, n;      // first: this lane's first head; rows_left: of its rows, kRows apart
+};
+template <int kRows>
+__device__ __forceinline__ RopeSegment rope_segment(const RopeParams& p, int token, int g, long long left, int row)
 {
-    if (kAdjacent) {
-        if (8 * part < rot) {
-            const float4 c = *reinterpret_cast<const float4*>(cs + 4 * part), s = *reinterpret_cast<const float4*>(sn + 4 * part);
-            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = y[2 * i], b = y[2 * i + 1];
-                y[2 * i] = a * cc[i] - b * ss[i];
-                y[2 * i + 1] = b * cc[i] + a * ss[i];
-            }
-        }
-    } else {
-        const int half = rot >> 4;               // lanes that hold the first halves of the pairs
-        const bool turns = part < 2 * half, lower = part < half;
-        const int partner = (int)ptx::lane_id() + (!turns ? 0 : lower ? half : -half);
-        float other[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) other[i] = __shfl_sync(0xffffffffu, y[i], partner);
-        if (turns) {
-            const int at = 8 * (lower ? part : part - half);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const float4 c = *reinterpret_cast<const float4*>(cs + at + 4 * q), s = *reinterpret_cast<const float4*>(sn + at + 4 * q);
-                const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float sg = lower ? -ss[i] : ss[i];
-                    y[4 * q + i] = y[4 * q + i] * cc[i] + other[4 * q + i] * sg;
-                }
-            }
-        }
-    }
+    const int kind = g < p.q_groups ? 0 : g < p.q_groups + p.k_groups ? 1 : 2;
+    const int from = g - (kind == 0 ? 0 : kind == 1 ? p.q_groups : p.q_groups + p.k_groups), here = kind == 0 ? p.q_groups : p.k_groups;
+    const int n = left < here - from ? (int)left : here - from, first = from * kRows + row;
+    const int heads = (kind == 0 ? p.H : p.kv_heads) - first, mine = n * kRows - row;
+    return {token, kind, first, heads < mine ? heads : mine, n};
 }
 
-// Forward.  Rows of a token in the order queries, keys, values; group g of kD / 8 lanes takes rows g, g + groups, ...
-template <int kD, int kBf16, int kAdjacent>
-__global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const RopeParams p)
-{
-    constexpr int kLanes = kD / 8, kGroups = kRopeThreads / kLanes, kAhead = 4;
-    __shared__ __align__(16) RopeShared<kD> s;
-    const int group = threadIdx.x / kLanes, part = threadIdx.x % kLanes;
-    const int t0 = blockIdx.x * p.tokens_per_cta;
-    const int n = p.T - t0 < p.tokens_per_cta ? p.T - t0 : p.tokens_per_cta;
-    const int rows = n * (int)p.rows.d;
-    float wq[8], wk[8];
-    bool ready = false;
-    for (int r0 = 0; r0 < rows; r0 += kAhead * kGroups) {
-        uint4 in[kAhead];
+template <int kRows, int kStreams>
+struct RopeStream {
+    RopeSegment seg;
+    const uint16_t* src[kStreams];
+    long long step[kStreams], left;     // left: row groups of the share not asked for yet
+    int token, g, row, lane_col;
+    __device__ __forceinline__ void open(const RopeParams& p) {
+        seg = rope_segment<kRows>(p, token, g, left, row);
+        g += seg.n;
+        if (g == p.groups) { g = 0; ++token; }
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int r = r0 + a * kGroups + group;
-            in[a] = make_uint4(0, 0, 0, 0);
-            if (r < rows) {
-                const int t = (int)p.rows.div((uint32_t)r), h = r - t * (int)p.rows.d;
-                const RopeTensor& x = h < p.H ? p.q : h < p.H + p.kv_heads ? p.k : p.v;
-                const int head = h < p.H ? h : h < p.H + p.kv_heads ? h - p.H : h - p.H - p.kv_heads;
-                in[a] = *reinterpret_cast<const uint4*>(x.p + (long long)(t0 + t) * x.token + (long long)head * x.head + 8 * part);
+        for (int s = 0; s < kStreams; ++s) {
+            const uint16_t* base = seg.kind == 0 ? (s ? p.dq_out.p : p.q.p) : seg.kind == 1 ? (s ? p.dk_out.p : p.k.p) : p.v.p;
+            const long long by_token = seg.kind == 0 ? (s ? p.dq_out.token : p.q.token) : seg.kind == 1 ? (s ? p.dk_out.token : p.k.token) : p.v.token;
+            const long long by_head = seg.kind == 0 ? (s ? p.dq_out.head : p.q.head) : seg.kind == 1 ? (s ? p.dk_out.head : p.k.head) : p.v.head;
+            src[s] = base + (long long)seg.token * by_token + (long long)seg.first * by_head + lane_col;
+            step[s] = by_head * kRows;
+        }
+    }
+    // Asks for the next row group (or nothing, behind the last) into `slot`.
+    __device__ __forceinline__ void ask(const RopeParams& p, uint32_t slot) {
+        if (left > 0) {
+            if (seg.n == 0) open(p);
+#pragma unroll
+            for (int s = 0; s < kStreams; ++s) {
+                cp_async16(slot + 512 * s, seg.rows_left > 0 ? src[s] : p.q.p, seg.rows_left > 0 ? 16 : 0);
+                src[s] += step[s];
             }
+            seg.rows_left -= kRows;
+            --seg.n;
+            --left;
         }
-        if (!ready) {
-            ready = true;
-            load_weight(p.q_weight, p.weight_f32, kBf16, 8 * part, wq);
-            load_weight(p.k_weight, p.weight_f32, kBf16, 8 * part, wk);
-            rope_prepare<kD>(p, s, t0, n, false);
-            __syncthreads();
-        }
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            // The whole warp stays in step for the shuffles; groups beyond the rows compute on zeros and store nothing.
-            const int r = r0 + a * kGroups + group;
-            if (!__any_sync(0xffffffffu, r < rows)) break;
-            const int rr = r < rows ? r : rows - 1;
-            const int t = (int)p.rows.div((uint32_t)rr), h = rr - t * (int)p.rows.d;
-            const bool is_q = h < p.H, is_v = h >= p.H + p.kv_heads;
-            const long long at = s.cache_at[t];
-            uint4 out = in[a];
-            float x[8];
-            unpack8<kBf16>(in[a], x);
-            float sq = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
-            sq = row_sum<kLanes>(sq);
-            const float scale = (is_q ? p.q_weight : p.k_weight) ? rsqrtf(sq * (1.f / kD) + p.eps) : 1.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * scale * (is_q ? wq[i] : wk[i]);
-            rotate_row<kD, kAdjacent>(x, s.cosine[t], s.sine[t], p.rot, part);
-            if (!is_v) out = pack8<kBf16>(x);
-            if (r < rows && at != -2) {
-                const int head = is_q ? h : is_v ? h - p.H - p.kv_heads : h - p.H;
-                if (is_q) {
-                    *reinterpret_cast<uint4*>(p.q_out.p + (long long)(t0 + t) * p.q_out.token + (long long)head * p.q_out.head + 8 * part) = out;
+        cp_async_commit();
+    }
+};
+
+// The weights of queries and of keys in the order of a lane's columns: u0 .. u3, v0 .. v3.
+template <int kD, int kBf16, int kAdjacent>
+__device__ __forceinline__ void rope_stage_weights(const RopeParams& p, float (&w)[2][kD])
+{
+    for (int i = threadIdx.x; i < 2 * kD; i += kRopeThreads) {
+        const int part = (i % kD) / 8, j = i % 8;
+        const RopeColumns<kAdjacent> col(p.rot, part);
+        w[i / kD][i % kD] = rope_weight(i < kD ? p.q_weight : p.k_weight, p.weight_f32, kBf16, j < 4 ? col.u(j) : col.v(j - 4));
+    }
+    __syncthreads();
+}
+
+// Forward.
+template <int kD, int kBf16, int kAdjacent>
+__global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_kernel(const RopeParams p)
+{
+    constexpr int kLanes = kD / 8, kRows = 32 / kLanes;
+    __shared__ __align__(16) uint8_t rings[kRopeWarps][kRopeDepth][512];
+    __shared__ __align__(16) float2 turns[kRopeWarps][kD / 2];
+    __shared__ __align__(16) float weights[2][kD];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
+    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
+    const RopeColumns<kAdjacent> col(p.rot, part);
+    long long begin, end;
+    rope_share(p, begin, end);
+    RopeStream<kRows, 1> stream;
+    stream.left = end - begin;
+    stream.token = (int)(begin / p.groups);
+    stream.g = (int)(begin - (long long)stream.token * p.groups);
+    stream.row = row;
+    stream.lane_col = 8 * part;
+    stream.seg.n = 0;
+    int token = stream.token, g = stream.g;
+    const uint32_t ring = ptx::smem_u32(rings[warp]) + 16 * lane;       // a row group as it lies in memory: rows of kLanes pieces
+#pragma unroll 1
+    for (int i = 0; i < kRopeDepth; ++i) stream.ask(p, ring + 512 * i);
+    int slot = 0, have_token = -1;
+    long long cache_at = -1;             // element offset of the token's first cache row; -1: none, -2: leave the token alone
+#pragma unroll 1
+    for (long long left = end - begin; left > 0;) {
+        RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
+        left -= seg.n;
+        if (token != have_token) {
+            have_token = token;
+            cache_at = -1;
+            if (p.slot) {
+                const long long at = p.slot[token];
+                if (at < 0) {
+                    cache_at = -2;
                 } else {
-                    if (!is_v && p.k_out.p)
-                        *reinterpret_cast<uint4*>(p.k_out.p + (long long)(t0 + t) * p.k_out.token + (long long)head * p.k_out.head + 8 * part) = out;
-                    if (at >= 0) {
-                        uint16_t* base = const_cast<uint16_t*>(is_v ? p.cache.v : p.cache.k);
-                        *reinterpret_cast<uint4*>(base + at + (long long)head * p.cache.head_stride + 8 * part) = out;
-                    }
+                    const long long page = at < 2147483648ll ? (long long)p.cache.page.div((uint32_t)at) : at / p.cache.page.d;
+                    if (page >= p.cache.num_pages) note_index(p.status, kIndexSlot);
+                    else cache_at = page * p.cache.page_stride + (at - page * p.cache.page.d) * p.cache.token_stride;
                 }
             }
+            if (seg.kind != 2) rope_angles(p, token, turns[warp]);
+        }
+        g += seg.n;
+        if (g == p.groups) { g = 0; ++token; }
+        const bool is_q = seg.kind == 0, is_v = seg.kind == 2;
+        uint16_t* const out_base = is_q ? p.q_out.p : p.k_out.p;
+        const long long out_head = is_q ? p.q_out.head : p.k_out.head;
+        uint16_t* out = out_base + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head;
+        uint16_t* cache = const_cast<uint16_t*>(is_v ? p.cache.v : p.cache.k) + cache_at + (long long)seg.first * p.cache.head_stride;
+        const long long out_step = out_head * kRows, cache_step = p.cache.head_stride * kRows;
+        const bool to_out = !is_v && out_base != nullptr && cache_at != -2, to_cache = !is_q && cache_at >= 0;
+        const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
+        ptx::f32x2 uc[2], vs[2], vc[2], us[2];        // wu cos, -wv sin, wv cos, wu sin
+        if (!is_v) {
+            const float4 wu = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part]), wv = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part + 4]);
+            float4 t0 = make_float4(1.f, 0.f, 1.f, 0.f), t1 = t0;      // cos, sin, cos, sin
+            if (col.turns) {
+                t0 = *reinterpret_cast<const float4*>(&turns[warp][4 * part]);
+                t1 = *reinterpret_cast<const float4*>(&turns[warp][4 * part + 2]);
+            }
+            uc[0] = ptx::pack_f32x2(wu.x * t0.x, wu.y * t0.z); uc[1] = ptx::pack_f32x2(wu.z * t1.x, wu.w * t1.z);
+            us[0] = ptx::pack_f32x2(wu.x * t0.y, wu.y * t0.w); us[1] = ptx::pack_f32x2(wu.z * t1.y, wu.w * t1.w);
+            vc[0] = ptx::pack_f32x2(wv.x * t0.x, wv.y * t0.z); vc[1] = ptx::pack_f32x2(wv.z * t1.x, wv.w * t1.z);
+            vs[0] = ptx::pack_f32x2(-wv.x * t0.y, -wv.y * t0.w); vs[1] = ptx::pack_f32x2(-wv.z * t1.y, -wv.w * t1.w);
+        }
+#pragma unroll 2
+        for (int i = 0; i < seg.n; ++i) {
+            cp_async_wait<kRopeDepth - 1>();
+            __syncwarp();
+            uint4 x = is_v ? *reinterpret_cast<const uint4*>(&rings[warp][slot][16 * lane])
+                           : col.load(reinterpret_cast<const uint16_t*>(&rings[warp][slot][2 * kD * row]));
+            __syncwarp();
+            stream.ask(p, ring + 512 * slot);
+            slot = slot + 1 == kRopeDepth ? 0 : slot + 1;
+            if (!is_v) {
+                ptx::f32x2 u[2], v[2], yu[2], yv[2];
+                rope_unpack<kBf16, kAdjacent>(x, u, v);
+                const float sum = pair_sum(ptx::add2(ptx::fma2(u[0], u[0], ptx::mul2(u[1], u[1])), ptx::fma2(v[0], v[0], ptx::mul2(v[1], v[1]))));
+                float r = rsqrtf(row_sum<kLanes>(sum) * (1.f / kD) + p.eps);
+                if (!normed) r = 1.f;
+                const ptx::f32x2 r2 = ptx::pack_f32x2(r, r);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    yu[j] = ptx::mul2(u[j], uc[j]);
+                    yv[j] = ptx::mul2(v[j], vc[j]);
+                    if (col.turns) {      // (0 * infinity must not reach columns that do not turn)
+                        yu[j] = ptx::fma2(v[j], vs[j], yu[j]);
+                        yv[j] = ptx::fma2(u[j], us[j], yv[j]);
+                    }
+                    yu[j] = ptx::mul2(yu[j], r2);
+                    yv[j] = ptx::mul2(yv[j], r2);
+                }
+                x = rope_pack<kBf16, kAdjacent>(yu, yv);
+            }
+            if (seg.rows_left > 0) {
+                if (to_out) col.store(out, x);
+                if (to_cache) {
+                    if (is_v) *reinterpret_cast<uint4*>(cache + 8 * part) = x;
+                    else col.store(cache, x);
+                }
+            }
+            out += out_step;
+            cache += cache_step;
+            seg.rows_left -= kRows;
         }
     }
+    cp_async_wait<0>();
 }
 
-// Backward.  A grid of resident CTAs walks the tokens; each lane keeps the weight sums of its eight columns over all of its
-// rows in registers (a few dozen rows), a CTA adds its groups' in a fixed order and leaves the sum in `partial`.
+// Backward: dn = R^T dy, g = dn w; with s = sum x^2 and t = sum g x over the row (one pass of shuffles for both), r = 1 / sqrt(s / d + eps),
+// dx = r (g - x r^2 t / d), dw += dn x r.  A lane keeps the weight sums of its eight columns over all of its rows (some dozens) in
+// registers; a CTA adds its warps' in a fixed order and leaves the sum in `partial`.
 template <int kD, int kBf16, int kAdjacent>
-__global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(const RopeParams p)
+__global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_bwd_kernel(const RopeParams p)
 {
-    constexpr int kLanes = kD / 8, kGroups = kRopeThreads / kLanes, kAhead = 2;
-    __shared__ __align__(16) RopeShared<kD> s;
-    __shared__ float sums[kGroups][kD];
-    const int group = threadIdx.x / kLanes, part = threadIdx.x % kLanes;
-    float wq[8], wk[8], aq[8] = {}, ak[8] = {};
-    load_weight(p.q_weight, p.weight_f32, kBf16, 8 * part, wq);
-    load_weight(p.k_weight, p.weight_f32, kBf16, 8 * part, wk);
-    for (long long t0l = (long long)blockIdx.x * p.tokens_per_cta; t0l < p.T; t0l += (long long)gridDim.x * p.tokens_per_cta) {
-        const int t0 = (int)t0l;
-        const int n = p.T - t0 < p.tokens_per_cta ? p.T - t0 : p.tokens_per_cta;
-        const int rows = n * (int)p.rows.d;
-        bool ready = false;
-        for (int r0 = 0; r0 < rows; r0 += kAhead * kGroups) {
-            uint4 in[kAhead], grad[kAhead];
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int r = r0 + a * kGroups + group;
-                in[a] = grad[a] = make_uint4(0, 0, 0, 0);
-                if (r < rows) {
-                    const int t = (int)p.rows.div((uint32_t)r), h = r - t * (int)p.rows.d;
-                    const RopeTensor& x = h < p.H ? p.q : p.k;
-                    const RopeTensor& g = h < p.H ? p.dq_out : p.dk_out;
-                    const int head = h < p.H ? h : h - p.H;
-                    in[a] = *reinterpret_cast<const uint4*>(x.p + (long long)(t0 + t) * x.token + (long long)head * x.head + 8 * part);
-                    grad[a] = *reinterpret_cast<const uint4*>(g.p + (long long)(t0 + t) * g.token + (long long)head * g.head + 8 * part);
-                }
-            }
-            if (!ready) {
-                ready = true;
-                __syncthreads();     // the last tokens' angles have been used
-                rope_prepare<kD>(p, s, t0, n, true);
-                __syncthreads();
-            }
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int r = r0 + a * kGroups + group;
-                if (!__any_sync(0xffffffffu, r < rows)) break;
-                const int rr = r < rows ? r : rows - 1;
-                const int t = (int)p.rows.div((uint32_t)rr), h = rr - t * (int)p.rows.d;
-                const bool is_q = h < p.H;
-                float x[8], y[8];
-                unpack8<kBf16>(in[a], x);
-                unpack8<kBf16>(grad[a], y);
-                rotate_row<kD, kAdjacent>(y, s.cosine[t], s.sine[t], p.rot, part);   // the sines are negated: R^T
-                // The sums are taken by whole warps, whether or not this lane's row has a weight.
-                const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
-                float sq = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
-                sq = row_sum<kLanes>(sq);
-                const float rs = rsqrtf(sq * (1.f / kD) + p.eps);
-                float dot = 0.f, g[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] *= rs;                             // x r
-                    g[i] = y[i] * (is_q ? wq[i] : wk[i]);
-                    dot = fmaf(g[i], x[i], dot);
-                }
-                dot = row_sum<kLanes>(dot) * (1.f / kD);
-                if (normed && r < rows) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float term = y[i] * x[i];     // dn x r
-                        if (is_q) aq[i] += term; else ak[i] += term;
-                        y[i] = rs * (g[i] - x[i] * dot);
-                    }
-                }
-                if (r < rows) {
-                    const RopeOut& o = is_q ? p.q_out : p.k_out;
-                    *reinterpret_cast<uint4*>(o.p + (long long)(t0 + t) * o.token + (long long)(is_q ? h : h - p.H) * o.head + 8 * part) = pack8<kBf16>(y);
-                }
+    constexpr int kLanes = kD / 8, kRows = 32 / kLanes;
+    __shared__ union {
+        __align__(16) uint8_t rings[kRopeWarps][kRopeBackwardDepth][1024];
+        float sums[kRopeWarps * kRows][kD];
+    } u_s;
+    __shared__ __align__(16) float2 turns[kRopeWarps][kD / 2];
+    __shared__ __align__(16) float weights[2][kD];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
+    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
+    const RopeColumns<kAdjacent> col(p.rot, part);
+    long long begin, end;
+    rope_share(p, begin, end);
+    RopeStream<kRows, 2> stream;
+    stream.left = end - begin;
+    stream.token = (int)(begin / p.groups);
+    stream.g = (int)(begin - (long long)stream.token * p.groups);
+    stream.row = row;
+    stream.lane_col = 8 * part;
+    stream.seg.n = 0;
+    int token = stream.token, g = stream.g;
+    const uint32_t ring = ptx::smem_u32(u_s.rings[warp]) + 16 * lane;
+#pragma unroll 1
+    for (int i = 0; i < kRopeBackwardDepth; ++i) stream.ask(p, ring + 1024 * i);
+    int slot = 0, have_token = -1;
+    const ptx::f32x2 zero = ptx::pack_f32x2(0.f, 0.f);
+    ptx::f32x2 dw[2][4] = {{zero, zero, zero, zero}, {zero, zero, zero, zero}};
+    ptx::f32x2 cs[2] = {zero, zero}, sn[2] = {zero, zero};
+#pragma unroll 1
+    for (long long left = end - begin; left > 0;) {
+        RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
+        left -= seg.n;
+        if (token != have_token) {
+            have_token = token;
+            rope_angles(p, token, turns[warp]);
+            if (col.turns) {
+                const float4 t0 = *reinterpret_cast<const float4*>(&turns[warp][4 * part]), t1 = *reinterpret_cast<const float4*>(&turns[warp][4 * part + 2]);
+                cs[0] = ptx::pack_f32x2(t0.x, t0.z); cs[1] = ptx::pack_f32x2(t1.x, t1.z);
+                sn[0] = ptx::pack_f32x2(t0.y, t0.w); sn[1] = ptx::pack_f32x2(t1.y, t1.w);
             }
         }
+        g += seg.n;
+        if (g == p.groups) { g = 0; ++token; }
+        const bool is_q = seg.kind == 0;
+        const long long out_head = is_q ? p.q_out.head : p.k_out.head, out_step = out_head * kRows;
+        uint16_t* out = (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head;
+        const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
+        const float4 wu4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part]), wv4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part + 4]);
+        const ptx::f32x2 wu[2] = {ptx::pack_f32x2(wu4.x, wu4.y), ptx::pack_f32x2(wu4.z, wu4.w)}, wv[2] = {ptx::pack_f32x2(wv4.x, wv4.y), ptx::pack_f32x2(wv4.z, wv4.w)};
+        ptx::f32x2 sum[4] = {zero, zero, zero, zero};      // of this segment: dn x r
+#pragma unroll 2
+        for (int i = 0; i < seg.n; ++i) {
+            cp_async_wait<kRopeBackwardDepth - 1>();
+            __syncwarp();
+            const uint4 in = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][2 * kD * row])),
+                        grad = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][512 + 2 * kD * row]));
+            __syncwarp();
+            stream.ask(p, ring + 1024 * slot);
+            slot = slot + 1 == kRopeBackwardDepth ? 0 : slot + 1;
+            ptx::f32x2 u[2], v[2], x[2], y[2];
+            rope_unpack<kBf16, kAdjacent>(grad, u, v);
+            if (col.turns) {           // R^T
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const ptx::f32x2 su = ptx::mul2(u[j], sn[j]);
+                    u[j] = ptx::fma2(u[j], cs[j], ptx::mul2(v[j], sn[j]));
+                    v[j] = ptx::sub2(ptx::mul2(v[j], cs[j]), su);
+                }
+            }
+            if (normed) {
+                rope_unpack<kBf16, kAdjacent>(in, x, y);
+                const ptx::f32x2 gu[2] = {ptx::mul2(u[0], wu[0]), ptx::mul2(u[1], wu[1])}, gv[2] = {ptx::mul2(v[0], wv[0]), ptx::mul2(v[1], wv[1])};
+                float s = pair_sum(ptx::add2(ptx::fma2(x[0], x[0], ptx::mul2(x[1], x[1])), ptx::fma2(y[0], y[0], ptx::mul2(y[1], y[1]))));
+                float t = pair_sum(ptx::add2(ptx::fma2(gu[0], x[0], ptx::mul2(gu[1], x[1])), ptx::fma2(gv[0], y[0], ptx::mul2(gv[1], y[1]))));
+                s = row_sum<kLanes>(s);
+                t = row_sum<kLanes>(t);
+                const float r = seg.rows_left > 0 ? rsqrtf(s * (1.f / kD) + p.eps) : 0.f;
+                const float m = -r * (r * t) * (1.f / kD);
+                const ptx::f32x2 r2 = ptx::pack_f32x2(r, r), m2 = ptx::pack_f32x2(m, m);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    sum[j] = ptx::fma2(u[j], ptx::mul2(x[j], r2), sum[j]);
+                    sum[2 + j] = ptx::fma2(v[j], ptx::mul2(y[j], r2), sum[2 + j]);
+                    u[j] = ptx::mul2(ptx::fma2(x[j], m2, gu[j]), r2);
+                    v[j] = ptx::mul2(ptx::fma2(y[j], m2, gv[j]), r2);
+                }
+            }
+            if (seg.rows_left > 0) col.store(out, rope_pack<kBf16, kAdjacent>(u, v));
+            out += out_step;
+            seg.rows_left -= kRows;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (is_q) dw[0][j] = ptx::add2(dw[0][j], sum[j]);
+            else dw[1][j] = ptx::add2(dw[1][j], sum[j]);
+        }
     }
+    cp_async_wait<0>();
+    float (*sums)[kD] = u_s.sums;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[group][8 * part + i] = which ? ak[i] : aq[i];
+        for (int i = 0; i < 4; ++i) {      // pairs (u0, u1), (u2, u3), (v0, v1), (v2, v3)
+            float lo, hi;
+            ptx::unpack_f32x2(dw[which][i], lo, hi);
+            const int k = 2 * (i & 1);
+            sums[warp * kRows + row][i < 2 ? col.u(k) : col.v(k)] = lo;
+            sums[warp * kRows + row][i < 2 ? col.u(k + 1) : col.v(k + 1)] = hi;
+        }
         __syncthreads();
         if (threadIdx.x < kD) {
             float a = 0.f;
-            for (int g = 0; g < kGroups; ++g) a += sums[g][threadIdx.x];
+            for (int g = 0; g < kRopeWarps * kRows; ++g) a += sums[g][threadIdx.x];
             p.partial[((long long)blockIdx.x * 2 + which) * kD + threadIdx.x] = a;
         }
     }
