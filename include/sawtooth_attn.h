@@ -331,7 +331,8 @@ int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* add
  * slot[t] < 0 (padding) is left alone altogether, q_out and k_out included; a slot beyond the cache is not written and noted in
  * the status word.  Two rows must not share a slot.  k_out may be NULL when there is a cache; v is needed exactly then.
  * rot_dim: 0 (no rotation; position and inv_freq may be NULL) or a multiple of 16 up to d.  T may be 0.  Weights: of `dtype`,
- * or fp32 (opts->weight_f32).  Base pointers 16-byte aligned, strides multiples of 8 elements.
+ * or fp32 (opts->weight_f32).  Base pointers 16-byte aligned, strides multiples of 8 elements, token strides below 2^31, head strides
+ * (the cache's too) at most 2^27.
  */
 typedef enum { ATTN_ROPE_HALVES = 0, ATTN_ROPE_ADJACENT = 1 } attn_rope_style;
 

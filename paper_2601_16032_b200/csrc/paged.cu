@@ -164,8 +164,16 @@ int rows_of(const char* name, const void* p, long long outer_stride, long long i
     *out = {p, outer, outer_stride * 2, inner, inner_stride * 2, (long long)d * 2};
     return ATTN_OK;
 }
-RopeTensor in_of(const Region& r) { return {static_cast<const uint16_t*>(r.p), r.outer_stride / 2, r.inner_stride / 2}; }
-RopeOut out_of(const Region& r) { return {static_cast<uint16_t*>(const_cast<void*>(r.p)), r.outer_stride / 2, r.inner_stride / 2}; }
+RopeTensor in_of(const Region& r) { return {static_cast<const uint16_t*>(r.p), (int)(r.outer_stride / 2), (int)(r.inner_stride / 2)}; }
+RopeOut out_of(const Region& r) { return {static_cast<uint16_t*>(const_cast<void*>(r.p)), (int)(r.outer_stride / 2), (int)(r.inner_stride / 2)}; }
+// The row kernels step by strides of 32 bits, the largest of them eight heads at a time.
+constexpr long long kMaxRowStride = 1ll << 27;
+int check_row_strides(const Region* r, int n) {
+    for (int i = 0; i < n; ++i)
+        if (r[i].p && ((r[i].outer > 1 && r[i].outer_stride / 2 > 16 * kMaxRowStride - 1) || (r[i].inner > 1 && r[i].inner_stride / 2 > kMaxRowStride)))
+            return fail(ATTN_ERR_INVALID_ARG, "token strides must be below 2^31 elements, head strides at most 2^27");
+    return ATTN_OK;
+}
 
 int check_rope(int T, int H, int kv_heads, int d, int dtype, const void* q_weight, const void* k_weight, float eps, const int* position,
                const double* inv_freq, int rot_dim, int rot_style, const attn_rope_opts& z) {
@@ -199,14 +207,14 @@ void fill_rope(RopeParams* p, int T, int H, int kv_heads, const void* q_weight, 
 }
 
 void rope_groups(RopeParams* p, int d, bool cached) {
-    const int rows = 32 / (d / 8);
+    const int rows = kRopeTwice * (32 / (d / 8));
     p->q_groups = (p->H + rows - 1) / rows;
     p->k_groups = (p->kv_heads + rows - 1) / rows;
     p->groups = p->q_groups + (cached ? 2 : 1) * p->k_groups;
 }
 // As many CTAs as are resident at a time, or as give every warp kRopeMinGroups row groups.
 int rope_grid(const RopeParams& p, int most) {
-    constexpr int kRopeMinGroups = 2;
+    constexpr int kRopeMinGroups = 1;
     const long long each = (long long)kRopeWarps * kRopeMinGroups, need = ((long long)p.T * p.groups + each - 1) / each;
     return need < 1 ? 1 : need < most ? (int)need : most;
 }
@@ -335,12 +343,16 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, 
         for (const Region& half : {span_of(c, c.k), span_of(c, c.v)})
             if (spans_overlap(half, rq) || spans_overlap(half, rk) || spans_overlap(half, rv) || spans_overlap(half, rqo) || spans_overlap(half, rko))
                 return fail(ATTN_ERR_INVALID_ARG, "the cache must not overlap the call's other arrays");
+        if (c.kv_heads > 1 && c.head_stride > kMaxRowStride) return fail(ATTN_ERR_INVALID_ARG, "the cache's head stride must be at most 2^27 elements");
         p.cache = view_of(c);
+        p.cache_head = c.kv_heads > 1 ? (int)c.head_stride : 0;
         p.slot = z.slot;
     }
     if ((overlap(rqo, rq) && !same(rqo, rq)) || overlap(rqo, rk) || overlap(rqo, rv) || overlap(rqo, rko) || (overlap(rko, rk) && !same(rko, rk)) ||
         overlap(rko, rq) || overlap(rko, rv))
         return fail(ATTN_ERR_INVALID_ARG, "q_out and k_out may be q and k themselves, but overlap nothing otherwise");
+    const Region rows[] = {rq, rk, rv, rqo, rko};
+    if ((rc = check_row_strides(rows, 5))) return rc;
     DeviceState ds;
     if ((rc = current_device(&ds, nullptr))) return rc;
     if (T == 0) return ATTN_OK;
@@ -385,6 +397,8 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
         overlap(rdk, rk) || overlap(rdk, rgq) || (overlap(rdk, rgk) && !same(rdk, rgk)) || overlap(ws, rq) || overlap(ws, rk) || overlap(ws, rgq) ||
         overlap(ws, rgk) || overlap(ws, rdq) || overlap(ws, rdk))
         return fail(ATTN_ERR_INVALID_ARG, "dq and dk may be dq_out and dk_out themselves, but overlap nothing otherwise");
+    const Region rows[] = {rq, rk, rgq, rgk, rdq, rdk};
+    if ((rc = check_row_strides(rows, 6))) return rc;
     DeviceState ds;
     if ((rc = current_device(&ds, nullptr))) return rc;
     fill_rope(&p, T, H, kv_heads, q_weight, k_weight, eps, position, inv_freq, rot_dim, z, ds);
@@ -510,10 +524,8 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
             if (overlap(outs[i], outs[j])) return fail(ATTN_ERR_INVALID_ARG, "o, lse and the workspace must not overlap");
     }
     DecodeParams p;
-    const RopeTensor tq = in_of(rq);
-    p.q = tq.p; p.q_request = tq.token; p.q_head = tq.head;
-    const RopeOut to = out_of(ro);
-    p.o = to.p; p.o_request = to.token; p.o_head = to.head;
+    p.q = static_cast<const uint16_t*>(q); p.q_request = rq.outer_stride / 2; p.q_head = rq.inner_stride / 2;
+    p.o = static_cast<uint16_t*>(o); p.o_request = ro.outer_stride / 2; p.o_head = ro.inner_stride / 2;
     p.lse = z.lse;
     p.cache = view_of(c);
     p.table = block_table;

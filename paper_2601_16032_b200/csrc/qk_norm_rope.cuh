@@ -3,7 +3,7 @@
 // All of it is one pass over memory, 4 d bytes a row (6 d backward), and an SM has some 60 warp instructions to spend on 512 bytes,
 // so it is the instructions that decide whether memory is kept busy.  A row is held by kD / 8 lanes, four rotated pairs each: with
 // halves as pairs a lane takes four columns from each half (two 8-byte loads), so that no lane needs another's columns; a
-// warp works on 32 / (kD / 8) rows of one token at a time.  Weight and rotation together are linear in the pair (u, v) and the same for all
+// warp works on twice 32 / (kD / 8) rows of one token at a time.  Weight and rotation together are linear in the pair (u, v) and the same for all
 // heads of a token:
 //     u' = r (u wu cos - v wv sin),   v' = r (v wv cos + u wu sin),   r = 1 / sqrt(mean x^2 + eps),
 // so a lane keeps the four products of its pairs in registers from head to head, and the arithmetic runs in packed pairs of
@@ -15,18 +15,19 @@
 
 namespace sawtooth {
 
-struct RopeTensor {      // rows of d elements
+// Rows of d elements; strides in elements, below 2^31 (an address is then one multiply-add per stride).
+struct RopeTensor {
     const uint16_t* p;
-    long long token, head;
+    int token, head;
 };
 struct RopeOut {
     uint16_t* p;
-    long long token, head;
+    int token, head;
 };
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kRopeForwardCtas = 3, kRopeBackwardCtas = 2, kRopeBackwardDepth = 4;   // CTAs of an SM, row groups asked for ahead
+constexpr int kRopeForwardCtas = 3, kRopeBackwardCtas = 2, kRopeBackwardDepth = 2;   // CTAs of an SM, row groups asked for ahead
 
 struct RopeParams {
     RopeTensor q, k, v;          // the projections
@@ -38,6 +39,7 @@ struct RopeParams {
     const double* inv_freq;
     const long long* slot;       // null: no cache
     CacheView cache;
+    int cache_head;              // its head stride
     float* partial;              // backward pass: [CTA][2][d] sums for the weights
     int* status;
     float eps;
@@ -46,11 +48,17 @@ struct RopeParams {
     int groups;                  // of a token in all
 };
 
+// (A 64-bit division takes a few hundred cycles, a 32-bit one a few dozen.)
+__device__ __forceinline__ long long rope_div(long long a, long long b)
+{
+    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // The row groups [begin, end) of the line that this warp takes.
 __device__ __forceinline__ void rope_share(const RopeParams& p, long long& begin, long long& end)
 {
     const long long total = (long long)p.T * p.groups, warps = (long long)gridDim.x * kRopeWarps, me = (long long)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-    const long long each = total / warps, more = total - each * warps;     // the first `more` warps take one more
+    const long long each = rope_div(total, warps), more = total - each * warps;     // the first `more` warps take one more
     begin = each * me + (me < more ? me : more);
     end = begin + each + (me < more ? 1 : 0);
 }
@@ -99,12 +107,12 @@ struct RopeColumns {
         const uint2 a = *reinterpret_cast<const uint2*>(row + c0), b = *reinterpret_cast<const uint2*>(row + c1);
         return make_uint4(a.x, a.y, b.x, b.y);
     }
-    __device__ __forceinline__ void store(uint16_t* row, const uint4& x) const {
+    __device__ __forceinline__ void store_at(uint16_t* first, const uint4& x) const {      // first: the row's column c0
         if (kAdjacent) {
-            *reinterpret_cast<uint4*>(row + c0) = x;
+            *reinterpret_cast<uint4*>(first) = x;
         } else {
-            *reinterpret_cast<uint2*>(row + c0) = make_uint2(x.x, x.y);
-            *reinterpret_cast<uint2*>(row + c1) = make_uint2(x.z, x.w);
+            *reinterpret_cast<uint2*>(first) = make_uint2(x.x, x.y);
+            *reinterpret_cast<uint2*>(first + (c1 - c0)) = make_uint2(x.z, x.w);
         }
     }
 };
@@ -150,18 +158,19 @@ __device__ __forceinline__ float row_sum(float x)
 
 // Rows reach a warp through a ring of its own in shared memory, filled kRopeDepth row groups ahead by 16-byte asynchronous copies, so that
 // what is in flight costs no registers.  RopeStream is the place that the copies have reached: kind by kind within a token.
-constexpr int kRopeDepth = 8;
+constexpr int kRopeDepth = 4;
+constexpr int kRopeTwice = 2;     // a row group is this many times as many rows as a warp holds at a time: the bookkeeping is shared by two
 
 struct RopeSegment {        // row groups of one token and kind that this warp takes
     int token, kind, first, rows_left, n;      // first: this lane's first head; rows_left: of its rows, kRows apart
 };
 template <int kRows>
-__device__ __forceinline__ RopeSegment rope_segment(const RopeParams& p, int token, int g, long long left, int row)
+__device__ __forceinline__ RopeSegment rope_segment(const RopeParams& p, int token, int g, int left, int row)
 {
     const int kind = g < p.q_groups ? 0 : g < p.q_groups + p.k_groups ? 1 : 2;
     const int from = g - (kind == 0 ? 0 : kind == 1 ? p.q_groups : p.q_groups + p.k_groups), here = kind == 0 ? p.q_groups : p.k_groups;
-    const int n = left < here - from ? (int)left : here - from, first = from * kRows + row;
-    const int heads = (kind == 0 ? p.H : p.kv_heads) - first, mine = n * kRows - row;
+    const int n = left < here - from ? left : here - from, first = from * kRows * kRopeTwice + row;
+    const int heads = (kind == 0 ? p.H : p.kv_heads) - first, mine = n * kRows * kRopeTwice - row;
     return {token, kind, first, heads < mine ? heads : mine, n};
 }
 
@@ -169,7 +178,8 @@ template <int kRows, int kStreams>
 struct RopeStream {
     RopeSegment seg;
     const uint16_t* src[kStreams];
-    long long step[kStreams], left;     // left: row groups of the share not asked for yet
+    int half[kStreams];                 // elements from a row to the one kRows heads on
+    int left;                           // row groups of the share not asked for yet
     int token, g, row, lane_col;
     __device__ __forceinline__ void open(const RopeParams& p) {
         seg = rope_segment<kRows>(p, token, g, left, row);
@@ -178,10 +188,10 @@ struct RopeStream {
 #pragma unroll
         for (int s = 0; s < kStreams; ++s) {
             const uint16_t* base = seg.kind == 0 ? (s ? p.dq_out.p : p.q.p) : seg.kind == 1 ? (s ? p.dk_out.p : p.k.p) : p.v.p;
-            const long long by_token = seg.kind == 0 ? (s ? p.dq_out.token : p.q.token) : seg.kind == 1 ? (s ? p.dk_out.token : p.k.token) : p.v.token;
-            const long long by_head = seg.kind == 0 ? (s ? p.dq_out.head : p.q.head) : seg.kind == 1 ? (s ? p.dk_out.head : p.k.head) : p.v.head;
+            const int by_token = seg.kind == 0 ? (s ? p.dq_out.token : p.q.token) : seg.kind == 1 ? (s ? p.dk_out.token : p.k.token) : p.v.token;
+            const int by_head = seg.kind == 0 ? (s ? p.dq_out.head : p.q.head) : seg.kind == 1 ? (s ? p.dk_out.head : p.k.head) : p.v.head;
             src[s] = base + (long long)seg.token * by_token + (long long)seg.first * by_head + lane_col;
-            step[s] = by_head * kRows;
+            half[s] = by_head * kRows;
         }
     }
     // Asks for the next row group (or nothing, behind the last) into `slot`.
@@ -190,10 +200,14 @@ struct RopeStream {
             if (seg.n == 0) open(p);
 #pragma unroll
             for (int s = 0; s < kStreams; ++s) {
-                cp_async16(slot + 512 * s, seg.rows_left > 0 ? src[s] : p.q.p, seg.rows_left > 0 ? 16 : 0);
-                src[s] += step[s];
+#pragma unroll
+                for (int h = 0; h < kRopeTwice; ++h) {
+                    const bool there = seg.rows_left > h * kRows;
+                    cp_async16(slot + 512 * (kRopeTwice * s + h), there ? src[s] + h * half[s] : p.q.p, there ? 16 : 0);
+                }
+                src[s] += kRopeTwice * half[s];
             }
-            seg.rows_left -= kRows;
+            seg.rows_left -= kRows * kRopeTwice;
             --seg.n;
             --left;
         }
@@ -218,17 +232,17 @@ template <int kD, int kBf16, int kAdjacent>
 __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_kernel(const RopeParams p)
 {
     constexpr int kLanes = kD / 8, kRows = 32 / kLanes;
-    __shared__ __align__(16) uint8_t rings[kRopeWarps][kRopeDepth][512];
+    __shared__ __align__(16) uint8_t rings[kRopeWarps][kRopeDepth][512 * kRopeTwice];
     __shared__ __align__(16) float2 turns[kRopeWarps][kD / 2];
     __shared__ __align__(16) float weights[2][kD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
-    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     const RopeColumns<kAdjacent> col(p.rot, part);
     long long begin, end;
     rope_share(p, begin, end);
     RopeStream<kRows, 1> stream;
-    stream.left = end - begin;
-    stream.token = (int)(begin / p.groups);
+    const int mine = (int)(end - begin);
+    stream.left = mine;
+    stream.token = (int)rope_div(begin, p.groups);
     stream.g = (int)(begin - (long long)stream.token * p.groups);
     stream.row = row;
     stream.lane_col = 8 * part;
@@ -236,11 +250,12 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
     int token = stream.token, g = stream.g;
     const uint32_t ring = ptx::smem_u32(rings[warp]) + 16 * lane;       // a row group as it lies in memory: rows of kLanes pieces
 #pragma unroll 1
-    for (int i = 0; i < kRopeDepth; ++i) stream.ask(p, ring + 512 * i);
+    for (int i = 0; i < kRopeDepth; ++i) stream.ask(p, ring + 512 * kRopeTwice * i);
+    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     int slot = 0, have_token = -1;
     long long cache_at = -1;             // element offset of the token's first cache row; -1: none, -2: leave the token alone
 #pragma unroll 1
-    for (long long left = end - begin; left > 0;) {
+    for (int left = mine; left > 0;) {
         RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
         left -= seg.n;
         if (token != have_token) {
@@ -260,13 +275,15 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
         }
         g += seg.n;
         if (g == p.groups) { g = 0; ++token; }
-        const bool is_q = seg.kind == 0, is_v = seg.kind == 2;
-        uint16_t* const out_base = is_q ? p.q_out.p : p.k_out.p;
-        const long long out_head = is_q ? p.q_out.head : p.k_out.head;
-        uint16_t* out = out_base + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head;
-        uint16_t* cache = const_cast<uint16_t*>(is_v ? p.cache.v : p.cache.k) + cache_at + (long long)seg.first * p.cache.head_stride;
-        const long long out_step = out_head * kRows, cache_step = p.cache.head_stride * kRows;
-        const bool to_out = !is_v && out_base != nullptr && cache_at != -2, to_cache = !is_q && cache_at >= 0;
+        // Where the rows go: queries to q_out, keys to k_out, to the cache or to both, values to the cache.
+        const bool is_q = seg.kind == 0, is_v = seg.kind == 2, dense = is_q || (!is_v && p.k_out.p != nullptr);
+        const bool to_out = dense ? cache_at != -2 : cache_at >= 0;
+        const bool to_both = dense && !is_q && cache_at >= 0;
+        uint16_t* cache = const_cast<uint16_t*>(is_v ? p.cache.v : p.cache.k) + cache_at + (long long)seg.first * p.cache_head + (is_v ? 8 * part : col.c0);
+        const int cache_half = p.cache_head * kRows;
+        const int out_head = is_q ? p.q_out.head : p.k_out.head, out_half = dense ? out_head * kRows : cache_half;
+        uint16_t* out = dense ? (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head + col.c0
+                              : cache;
         const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
         ptx::f32x2 uc[2], vs[2], vc[2], us[2];        // wu cos, -wv sin, wv cos, wu sin
         if (!is_v) {
@@ -281,45 +298,54 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
             vc[0] = ptx::pack_f32x2(wv.x * t0.x, wv.y * t0.z); vc[1] = ptx::pack_f32x2(wv.z * t1.x, wv.w * t1.z);
             vs[0] = ptx::pack_f32x2(-wv.x * t0.y, -wv.y * t0.w); vs[1] = ptx::pack_f32x2(-wv.z * t1.y, -wv.w * t1.w);
         }
-#pragma unroll 2
+#pragma unroll 1
         for (int i = 0; i < seg.n; ++i) {
             cp_async_wait<kRopeDepth - 1>();
             __syncwarp();
-            uint4 x = is_v ? *reinterpret_cast<const uint4*>(&rings[warp][slot][16 * lane])
-                           : col.load(reinterpret_cast<const uint16_t*>(&rings[warp][slot][2 * kD * row]));
+            uint4 x[kRopeTwice];
+#pragma unroll
+            for (int h = 0; h < kRopeTwice; ++h)
+                x[h] = is_v ? *reinterpret_cast<const uint4*>(&rings[warp][slot][512 * h + 16 * lane])
+                            : col.load(reinterpret_cast<const uint16_t*>(&rings[warp][slot][512 * h + 2 * kD * row]));
             __syncwarp();
-            stream.ask(p, ring + 512 * slot);
+            stream.ask(p, ring + 512 * kRopeTwice * slot);
             slot = slot + 1 == kRopeDepth ? 0 : slot + 1;
             if (!is_v) {
-                ptx::f32x2 u[2], v[2], yu[2], yv[2];
-                rope_unpack<kBf16, kAdjacent>(x, u, v);
-                const float sum = pair_sum(ptx::add2(ptx::fma2(u[0], u[0], ptx::mul2(u[1], u[1])), ptx::fma2(v[0], v[0], ptx::mul2(v[1], v[1]))));
-                float r = rsqrtf(row_sum<kLanes>(sum) * (1.f / kD) + p.eps);
-                if (!normed) r = 1.f;
-                const ptx::f32x2 r2 = ptx::pack_f32x2(r, r);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    yu[j] = ptx::mul2(u[j], uc[j]);
-                    yv[j] = ptx::mul2(v[j], vc[j]);
-                    if (col.turns) {      // (0 * infinity must not reach columns that do not turn)
-                        yu[j] = ptx::fma2(v[j], vs[j], yu[j]);
-                        yv[j] = ptx::fma2(u[j], us[j], yv[j]);
+                for (int h = 0; h < kRopeTwice; ++h) {
+                    ptx::f32x2 u[2], v[2], yu[2], yv[2];
+                    rope_unpack<kBf16, kAdjacent>(x[h], u, v);
+                    const float sum = pair_sum(ptx::add2(ptx::fma2(u[0], u[0], ptx::mul2(u[1], u[1])), ptx::fma2(v[0], v[0], ptx::mul2(v[1], v[1]))));
+                    float r = rsqrtf(row_sum<kLanes>(sum) * (1.f / kD) + p.eps);
+                    if (!normed) r = 1.f;
+                    const ptx::f32x2 r2 = ptx::pack_f32x2(r, r);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        yu[j] = ptx::mul2(u[j], uc[j]);
+                        yv[j] = ptx::mul2(v[j], vc[j]);
+                        if (col.turns) {      // (0 * infinity must not reach columns that do not turn)
+                            yu[j] = ptx::fma2(v[j], vs[j], yu[j]);
+                            yv[j] = ptx::fma2(u[j], us[j], yv[j]);
+                        }
+                        yu[j] = ptx::mul2(yu[j], r2);
+                        yv[j] = ptx::mul2(yv[j], r2);
                     }
-                    yu[j] = ptx::mul2(yu[j], r2);
-                    yv[j] = ptx::mul2(yv[j], r2);
-                }
-                x = rope_pack<kBf16, kAdjacent>(yu, yv);
-            }
-            if (seg.rows_left > 0) {
-                if (to_out) col.store(out, x);
-                if (to_cache) {
-                    if (is_v) *reinterpret_cast<uint4*>(cache + 8 * part) = x;
-                    else col.store(cache, x);
+                    x[h] = rope_pack<kBf16, kAdjacent>(yu, yv);
                 }
             }
-            out += out_step;
-            cache += cache_step;
-            seg.rows_left -= kRows;
+            if (to_out) {
+#pragma unroll
+                for (int h = 0; h < kRopeTwice; ++h) {
+                    if (seg.rows_left > h * kRows) {
+                        if (is_v) *reinterpret_cast<uint4*>(out + h * out_half) = x[h];
+                        else col.store_at(out + h * out_half, x[h]);
+                        if (to_both) col.store_at(cache + h * cache_half, x[h]);
+                    }
+                }
+            }
+            out += kRopeTwice * out_half;
+            cache += kRopeTwice * cache_half;
+            seg.rows_left -= kRows * kRopeTwice;
         }
     }
     cp_async_wait<0>();
@@ -333,19 +359,19 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
 {
     constexpr int kLanes = kD / 8, kRows = 32 / kLanes;
     __shared__ union {
-        __align__(16) uint8_t rings[kRopeWarps][kRopeBackwardDepth][1024];
+        __align__(16) uint8_t rings[kRopeWarps][kRopeBackwardDepth][1024 * kRopeTwice];
         float sums[kRopeWarps * kRows][kD];
     } u_s;
     __shared__ __align__(16) float2 turns[kRopeWarps][kD / 2];
     __shared__ __align__(16) float weights[2][kD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
-    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     const RopeColumns<kAdjacent> col(p.rot, part);
     long long begin, end;
     rope_share(p, begin, end);
     RopeStream<kRows, 2> stream;
-    stream.left = end - begin;
-    stream.token = (int)(begin / p.groups);
+    const int mine = (int)(end - begin);
+    stream.left = mine;
+    stream.token = (int)rope_div(begin, p.groups);
     stream.g = (int)(begin - (long long)stream.token * p.groups);
     stream.row = row;
     stream.lane_col = 8 * part;
@@ -353,13 +379,14 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
     int token = stream.token, g = stream.g;
     const uint32_t ring = ptx::smem_u32(u_s.rings[warp]) + 16 * lane;
 #pragma unroll 1
-    for (int i = 0; i < kRopeBackwardDepth; ++i) stream.ask(p, ring + 1024 * i);
+    for (int i = 0; i < kRopeBackwardDepth; ++i) stream.ask(p, ring + 1024 * kRopeTwice * i);
+    rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     int slot = 0, have_token = -1;
     const ptx::f32x2 zero = ptx::pack_f32x2(0.f, 0.f);
     ptx::f32x2 dw[2][4] = {{zero, zero, zero, zero}, {zero, zero, zero, zero}};
     ptx::f32x2 cs[2] = {zero, zero}, sn[2] = {zero, zero};
 #pragma unroll 1
-    for (long long left = end - begin; left > 0;) {
+    for (int left = mine; left > 0;) {
         RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
         left -= seg.n;
         if (token != have_token) {
@@ -374,52 +401,60 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
         g += seg.n;
         if (g == p.groups) { g = 0; ++token; }
         const bool is_q = seg.kind == 0;
-        const long long out_head = is_q ? p.q_out.head : p.k_out.head, out_step = out_head * kRows;
-        uint16_t* out = (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head;
+        const int out_head = is_q ? p.q_out.head : p.k_out.head, out_half = out_head * kRows;
+        uint16_t* out = (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head + col.c0;
         const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
         const float4 wu4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part]), wv4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part + 4]);
         const ptx::f32x2 wu[2] = {ptx::pack_f32x2(wu4.x, wu4.y), ptx::pack_f32x2(wu4.z, wu4.w)}, wv[2] = {ptx::pack_f32x2(wv4.x, wv4.y), ptx::pack_f32x2(wv4.z, wv4.w)};
         ptx::f32x2 sum[4] = {zero, zero, zero, zero};      // of this segment: dn x r
-#pragma unroll 2
+#pragma unroll 1
         for (int i = 0; i < seg.n; ++i) {
             cp_async_wait<kRopeBackwardDepth - 1>();
             __syncwarp();
-            const uint4 in = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][2 * kD * row])),
-                        grad = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][512 + 2 * kD * row]));
+            uint4 in[kRopeTwice], grad[kRopeTwice];
+#pragma unroll
+            for (int h = 0; h < kRopeTwice; ++h) {
+                in[h] = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][512 * h + 2 * kD * row]));
+                grad[h] = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][512 * (kRopeTwice + h) + 2 * kD * row]));
+            }
             __syncwarp();
-            stream.ask(p, ring + 1024 * slot);
+            stream.ask(p, ring + 1024 * kRopeTwice * slot);
             slot = slot + 1 == kRopeBackwardDepth ? 0 : slot + 1;
-            ptx::f32x2 u[2], v[2], x[2], y[2];
-            rope_unpack<kBf16, kAdjacent>(grad, u, v);
-            if (col.turns) {           // R^T
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const ptx::f32x2 su = ptx::mul2(u[j], sn[j]);
-                    u[j] = ptx::fma2(u[j], cs[j], ptx::mul2(v[j], sn[j]));
-                    v[j] = ptx::sub2(ptx::mul2(v[j], cs[j]), su);
-                }
-            }
-            if (normed) {
-                rope_unpack<kBf16, kAdjacent>(in, x, y);
-                const ptx::f32x2 gu[2] = {ptx::mul2(u[0], wu[0]), ptx::mul2(u[1], wu[1])}, gv[2] = {ptx::mul2(v[0], wv[0]), ptx::mul2(v[1], wv[1])};
-                float s = pair_sum(ptx::add2(ptx::fma2(x[0], x[0], ptx::mul2(x[1], x[1])), ptx::fma2(y[0], y[0], ptx::mul2(y[1], y[1]))));
-                float t = pair_sum(ptx::add2(ptx::fma2(gu[0], x[0], ptx::mul2(gu[1], x[1])), ptx::fma2(gv[0], y[0], ptx::mul2(gv[1], y[1]))));
-                s = row_sum<kLanes>(s);
-                t = row_sum<kLanes>(t);
-                const float r = seg.rows_left > 0 ? rsqrtf(s * (1.f / kD) + p.eps) : 0.f;
-                const float m = -r * (r * t) * (1.f / kD);
-                const ptx::f32x2 r2 = ptx::pack_f32x2(r, r), m2 = ptx::pack_f32x2(m, m);
+            for (int h = 0; h < kRopeTwice; ++h) {
+                ptx::f32x2 u[2], v[2], x[2], y[2];
+                rope_unpack<kBf16, kAdjacent>(grad[h], u, v);
+                if (col.turns) {           // R^T
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    sum[j] = ptx::fma2(u[j], ptx::mul2(x[j], r2), sum[j]);
-                    sum[2 + j] = ptx::fma2(v[j], ptx::mul2(y[j], r2), sum[2 + j]);
-                    u[j] = ptx::mul2(ptx::fma2(x[j], m2, gu[j]), r2);
-                    v[j] = ptx::mul2(ptx::fma2(y[j], m2, gv[j]), r2);
+                    for (int j = 0; j < 2; ++j) {
+                        const ptx::f32x2 su = ptx::mul2(u[j], sn[j]);
+                        u[j] = ptx::fma2(u[j], cs[j], ptx::mul2(v[j], sn[j]));
+                        v[j] = ptx::sub2(ptx::mul2(v[j], cs[j]), su);
+                    }
                 }
+                const bool there = seg.rows_left > h * kRows;
+                if (normed) {
+                    rope_unpack<kBf16, kAdjacent>(in[h], x, y);
+                    const ptx::f32x2 gu[2] = {ptx::mul2(u[0], wu[0]), ptx::mul2(u[1], wu[1])}, gv[2] = {ptx::mul2(v[0], wv[0]), ptx::mul2(v[1], wv[1])};
+                    float s = pair_sum(ptx::add2(ptx::fma2(x[0], x[0], ptx::mul2(x[1], x[1])), ptx::fma2(y[0], y[0], ptx::mul2(y[1], y[1]))));
+                    float t = pair_sum(ptx::add2(ptx::fma2(gu[0], x[0], ptx::mul2(gu[1], x[1])), ptx::fma2(gv[0], y[0], ptx::mul2(gv[1], y[1]))));
+                    s = row_sum<kLanes>(s);
+                    t = row_sum<kLanes>(t);
+                    const float r = there ? rsqrtf(s * (1.f / kD) + p.eps) : 0.f;
+                    const float m = -r * (r * t) * (1.f / kD);
+                    const ptx::f32x2 r2 = ptx::pack_f32x2(r, r), m2 = ptx::pack_f32x2(m, m);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        sum[j] = ptx::fma2(u[j], ptx::mul2(x[j], r2), sum[j]);
+                        sum[2 + j] = ptx::fma2(v[j], ptx::mul2(y[j], r2), sum[2 + j]);
+                        u[j] = ptx::mul2(ptx::fma2(x[j], m2, gu[j]), r2);
+                        v[j] = ptx::mul2(ptx::fma2(y[j], m2, gv[j]), r2);
+                    }
+                }
+                if (there) col.store_at(out + h * out_half, rope_pack<kBf16, kAdjacent>(u, v));
             }
-            if (seg.rows_left > 0) col.store(out, rope_pack<kBf16, kAdjacent>(u, v));
-            out += out_step;
-            seg.rows_left -= kRows;
+            out += kRopeTwice * out_half;
+            seg.rows_left -= kRows * kRopeTwice;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

@@ -69,7 +69,7 @@ COMMON = [
     (dict(q=0), -1), (dict(k=0), -1), (dict(q_out=0), -1), (dict(T=-1), -1), (dict(H=0), -1), (dict(Hk=0), -1), (dict(d=96), -2), (dict(dtype=2), -1),
     (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1), (dict(rot=8), -1), (dict(rot=144), -1), (dict(rot=-16), -1),
     (dict(style=2), -1), (dict(position=0), -1), (dict(freq=0), -1), (dict(freq=at(8) + 4), -3), (dict(wq=at(5) + 2), -3), (dict(q=at(0) + 8), -3),
-    (dict(opts=dict(q_token=4)), -1), (dict(opts=dict(q_token=-8)), -1), (dict(opts=dict(q_token=1 << 60)), -1), (dict(opts=dict(weight_f32=2)), -1),
+    (dict(opts=dict(q_token=4)), -1), (dict(opts=dict(q_token=-8)), -1), (dict(opts=dict(q_token=1 << 60)), -1), (dict(opts=dict(k_token=1 << 31, k_head=128)), -1), (dict(opts=dict(q_token=128, q_head=1 << 28)), -1), (dict(opts=dict(weight_f32=2)), -1),
     (dict(opts=dict(check_mode=3)), -1)]
 
 
@@ -86,7 +86,7 @@ def test_rope_forward(change, status):
     (dict(kv_heads=4), {}, -1), (dict(d=64), {}, -1), (dict(dtype=sa.F16), {}, -1), (dict(layout=2), {}, -1), (dict(k=at(14) + 2), {}, -3),
     (dict(page_stride=4096, token_stride=256, head_stride=100), {}, -1), (dict(page_stride=4096, token_stride=128, head_stride=128), {}, -1),
     (dict(page_stride=2048, token_stride=256, head_stride=128), {}, -1), (dict(page_stride=-4096, token_stride=256, head_stride=128), {}, -1),
-    (dict(page_stride=1 << 54, token_stride=256, head_stride=128), {}, -1), ({}, dict(v=0), -1), ({}, dict(slot=0), -1), ({}, dict(slot=at(16) + 4), -3),
+    (dict(page_stride=1 << 54, token_stride=256, head_stride=128), {}, -1), (dict(page_stride=1 << 30, token_stride=128, head_stride=1 << 28), {}, -1), ({}, dict(v=0), -1), ({}, dict(slot=0), -1), ({}, dict(slot=at(16) + 4), -3),
     (dict(k=at(3)), {}, -1), (dict(v=at(0)), {}, -1)])
 def test_rope_cache(cache, more, status):
     refused(rope_call(cache=cache, v=more.get("v", at(2)), opts=dict(slot=more.get("slot", at(16)))), status)
