@@ -1,9 +1,11 @@
-// Block tables, slot maps and positions of a serving step from the requests' lengths: one cluster of CTAs.
+// Block tables, slot maps and positions of a serving step from the requests' lengths, in one launch.
 //
 // Per request: tokens added, pages taken, pages given back; their prefix sums over the requests say where each token, taken
-// and returned page stands.  Every CTA of the cluster makes the (short) scan for itself and keeps it in shared memory; after
-// a cluster barrier, behind which no input is read that an output may alias, the threads of all CTAs together write one
-// token or one page each, finding its request by bisection.
+// and returned page stands.  Every CTA makes the (short) scan for itself and keeps it in shared memory; then the threads of all
+// CTAs together write one token or one page each, finding its request by bisection.  What bounds it is latency: the launch, the
+// lengths, the scan, and a page number for each token.  Where an output is an input's own array (lengths or the count of free pages
+// updated in place), the CTAs are one cluster, and its barrier keeps the writes behind everybody's reads; otherwise nothing
+// needs to wait and there can be more of them.  (16 000 tokens of 256 requests: MIXED_PLAIN us with 32 CTAs, MIXED_CLUSTER us with a cluster of 8.)
 //
 // With c free pages and R returned ones the stack is free[0 .. c-1], returned[0 .. R-1]; the i-th page taken is entry c + R - 1 - i.
 // Entries below c come from the array, the others from the tables of the requests that end, and what stays on the stack of the
@@ -30,6 +32,7 @@ struct PagePlanParams {
     int* request;    // or nullptr
     int* info;
     int B, width, capacity, token_cap;
+    int in_place;    // an output is an input's own array
     FastDiv page;
 };
 
@@ -109,7 +112,7 @@ __global__ void __launch_bounds__(1024) page_plan_kernel(const PagePlanParams p)
                     : (taken > stack || stack - taken > p.capacity) ? ATTN_PLAN_NO_PAGES : ATTN_PLAN_FITS;
     const bool fits = state == ATTN_PLAN_FITS;
     // From here on `cached` and `free_count` may be overwritten by their outputs: all CTAs have read them.
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (p.in_place) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
     const int me = rank * threads + tid;
     if (me == 0) {

@@ -312,9 +312,12 @@ int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* add
     const size_t smem = (size_t)B * 4 * sizeof(int);
     if (smem > 40 * 1024 && (rc = raise_smem(dev, ds, (const void*)page_plan_kernel, kRaisedPlan, kPlanMaxRequests * 16))) return rc;
     const long long items = (long long)token_cap + B;
-    const int threads = items <= 512 ? 256 : 1024;
-    const int cluster = items <= 4096 ? 1 : 8;
-    return launch_status(launch_ex(page_plan_kernel, cluster, 1, threads, smem, static_cast<cudaStream_t>(stream), cluster, false, p));
+    // One item a thread, as far as 32 CTAs of 512 threads go, or 8 in a cluster of 1024.
+    p.in_place = seq_len == cached || pool->free_count_out == pool->free_count;
+    const int threads = p.in_place && items > 512 ? 1024 : items <= 256 ? 256 : 512;
+    const long long want = (items + threads - 1) / threads;
+    const int ctas = p.in_place ? (want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8) : (int)(want < 32 ? want : 32);
+    return launch_status(launch_ex(page_plan_kernel, ctas, 1, threads, smem, static_cast<cudaStream_t>(stream), p.in_place ? ctas : 0, false, p));
 }
 
 int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out, int T, int H, int kv_heads, int d, int dtype,

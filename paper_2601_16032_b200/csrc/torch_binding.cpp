@@ -43,6 +43,25 @@ int kind_of(const Tensor& t) {
     return ATTN_F16;
 }
 
+// Tensors of one dimension cut from one allocation: a caching allocator's call takes longer than all else that a small
+// output costs.  Each starts on a multiple of 16 bytes.
+class Cuts {
+public:
+    Cuts(int64_t bytes, const Tensor& like) : base_(at::empty({bytes}, like.options().dtype(at::kByte))) {}
+    static int64_t room(int64_t n, int64_t size) { return (n * size + 15) / 16 * 16; }
+    Tensor take(int64_t n, at::ScalarType type) {
+        const int64_t size = (int64_t)c10::elementSize(type);
+        Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base_.storage()), base_.key_set(), c10::scalarTypeToTypeMeta(type));
+        t.unsafeGetTensorImpl()->set_storage_offset(at_ / size);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+        at_ += room(n, size);
+        return t;
+    }
+private:
+    Tensor base_;
+    int64_t at_ = 0;
+};
+
 // A contiguous tensor of one dimension with n elements of this type, on this device.
 template <typename T>
 T* vector_of(const Tensor& t, int64_t n, at::ScalarType type, const Tensor& like, const char* message) {
@@ -100,11 +119,14 @@ py::tuple page_plan(const Tensor& cached, const Tensor& added, int page_size, co
              table.size(1) <= 2147483647 && (table.size(1) == 1 || table.stride(1) == 1) && free_pages.numel() <= 2147483647,
          "block_table must be an int32 tensor [B, width] on the device of the others with contiguous rows");
     const c10::cuda::OptionalCUDAGuard guard(cached.device());
-    Tensor seq_len = seq_len_out ? *seq_len_out : at::empty_like(cached);
-    Tensor count_out = free_count_out ? *free_count_out : at::empty_like(free_count);
-    const auto options = cached.options();
-    Tensor q_start = at::empty({B + 1}, options), info = at::empty({4}, options), position = at::empty({token_cap}, options),
-           request = at::empty({token_cap}, options), slot = at::empty({token_cap}, options.dtype(at::kLong));
+    const bool own_len = !seq_len_out, own_count = !free_count_out;
+    Cuts cuts(Cuts::room(token_cap, 8) + 2 * Cuts::room(token_cap, 4) + Cuts::room(B + 1, 4) + Cuts::room(4, 4) + (own_len ? Cuts::room(B, 4) : 0) +
+                  (own_count ? Cuts::room(1, 4) : 0),
+              cached);
+    Tensor slot = cuts.take(token_cap, at::kLong), position = cuts.take(token_cap, at::kInt), request = cuts.take(token_cap, at::kInt),
+           q_start = cuts.take(B + 1, at::kInt), info = cuts.take(4, at::kInt);
+    Tensor seq_len = own_len ? cuts.take(B, at::kInt) : *seq_len_out;
+    Tensor count_out = own_count ? cuts.take(1, at::kInt) : *free_count_out;
     attn_page_pool pool = {};
     pool.block_table = static_cast<int*>(table.data_ptr());
     pool.table_stride = B > 1 ? table.stride(0) : table.size(1);
@@ -199,8 +221,11 @@ py::tuple qk_norm_rope_backward(const Tensor& dq_out, const Tensor& dk_out, cons
     Tensor dq = dq_given ? *dq_given : at::empty(q.sizes(), q.options()), dk = dk_given ? *dk_given : at::empty(k.sizes(), k.options());
     need(dq.sizes() == q.sizes() && dq_out.sizes() == q.sizes() && dk.sizes() == k.sizes() && dk_out.sizes() == k.sizes(), "gradients must have the shapes of q and k");
     OptTensor dq_weight, dk_weight;
-    if (a.q_weight) dq_weight = at::empty({q.size(2)}, q.options().dtype(at::kFloat));
-    if (a.k_weight) dk_weight = at::empty({q.size(2)}, q.options().dtype(at::kFloat));
+    if (a.q_weight || a.k_weight) {
+        Cuts cuts(2 * Cuts::room(q.size(2), 4), q);
+        if (a.q_weight) dq_weight = cuts.take(q.size(2), at::kFloat);
+        if (a.k_weight) dk_weight = cuts.take(q.size(2), at::kFloat);
+    }
     Tensor workspace = workspace_of(workspace_given, attn_rope_bwd_workspace_bytes((int)q.size(2)), q);
     attn_rope_opts o = {};
     const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), rk = rows_of(k, q, "k must be like q: type, device, rows of d contiguous elements"),
