@@ -377,7 +377,8 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
  *
  * The work is cut over the length: the tiles (64 tokens; 128 at d = 64) of all requests and K/V heads, in that order, are dealt out to the CTAs in equal
  * contiguous shares whatever the lengths (attn_decode_trace replays it), and requests cut by a share's border are joined by
- * their running maxima and sums.  For fixed arguments bitwise reproducible.  The products take their 16-bit operands as they are;
+ * their running maxima and sums.  Where the tables are so short, and the requests so few, that each request and K/V head can have a few
+ * CTAs with a few tiles each (attn_decode_plan.cluster), they take the request's tiles between them instead.  For fixed arguments bitwise reproducible.  The products take their 16-bit operands as they are;
  * probabilities enter the second product as the sum of two 16-bit numbers; sums are fp32; o is rounded once.
  *
  * q, o: [B, H, d], strides in opts, d elements contiguous, 16-byte aligned, strides multiples of 8.  o must not overlap q, the
@@ -397,6 +398,7 @@ typedef struct {
     int tile_tokens;         /* tokens of a tile */
     int head_blocks;         /* blocks of up to 32 query heads that read one K/V head */
     int min_tiles;           /* a CTA's share is at least this many tiles (but for rounding) */
+    int cluster;             /* CTAs that work on a request's head block in the form for short requests; 0: even shares */
     size_t workspace_bytes;
 } attn_decode_plan;
 
@@ -409,8 +411,12 @@ typedef struct {
     int first_cta, last_cta;    /* CTAs that share the request's tiles of this head */
 } attn_decode_trace_entry;
 
-/* What a call will launch.  sm_count <= 0 asks the current device. */
-int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count, attn_decode_plan* out);
+/*
+ * What a call will launch: with max_tokens = max_pages * page_size, the most tokens a request can have (0: not looked at, even shares).
+ * sm_count <= 0 asks the current device.
+ */
+int attn_decode_query_plan(int B, int H, int kv_heads, int d, long long max_tokens, const attn_decode_opts* opts, int sm_count,
+                           attn_decode_plan* out);
 int attn_decode_trace(const int* seq_len_host, int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count,
                       attn_decode_trace_entry* buf, size_t cap, size_t* n);
 

@@ -88,7 +88,7 @@ class DecodeOpts(ctypes.Structure):
 
 
 class DecodePlan(ctypes.Structure):
-    _fields_ = [(name, ctypes.c_int) for name in ("grid", "threads", "smem_bytes", "tile_tokens", "head_blocks", "min_tiles")] + [
+    _fields_ = [(name, ctypes.c_int) for name in ("grid", "threads", "smem_bytes", "tile_tokens", "head_blocks", "min_tiles", "cluster")] + [
         ("workspace_bytes", ctypes.c_size_t)]
 
 
@@ -135,7 +135,7 @@ def load_library():
     lib.attn_rope_bwd_workspace_bytes.argtypes = [ci]
     lib.attn_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
     lib.attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [ci] * 5 + [vp, vp, cf, vp, vp, ci, ci, vp, ctypes.c_size_t, vp, ctypes.POINTER(RopeOpts)]
-    lib.attn_decode_query_plan.argtypes = [ci, ci, ci, ci, ctypes.POINTER(DecodeOpts), ci, ctypes.POINTER(DecodePlan)]
+    lib.attn_decode_query_plan.argtypes = [ci, ci, ci, ci, ctypes.c_longlong, ctypes.POINTER(DecodeOpts), ci, ctypes.POINTER(DecodePlan)]
     lib.attn_decode_trace.argtypes = [ctypes.POINTER(ci), ci, ci, ci, ci, ctypes.POINTER(DecodeOpts), ci, ctypes.POINTER(DecodeTraceEntry), ctypes.c_size_t,
                                       ctypes.POINTER(ctypes.c_size_t)]
     lib.attn_decode_paged.argtypes = [vp, ctypes.POINTER(KVCache), vp, ctypes.c_longlong, ci, vp, vp, ci, ci, cf, vp, ctypes.c_size_t, vp,
@@ -267,9 +267,9 @@ def attn_qk_norm_rope_bwd(dq_out: int, dk_out: int, q: int, k: int, dq: int, dk:
                                                 position, inv_freq, rot_dim, rot_style, workspace, workspace_bytes, stream, _opts_ptr(opts)))
 
 
-def attn_decode_query_plan(B: int, H: int, kv_heads: int, d: int, opts: Optional[DecodeOpts] = None, sm_count: int = 0) -> DecodePlan:
+def attn_decode_query_plan(B: int, H: int, kv_heads: int, d: int, max_tokens: int = 0, opts: Optional[DecodeOpts] = None, sm_count: int = 0) -> DecodePlan:
     plan = DecodePlan()
-    _check(load_library().attn_decode_query_plan(B, H, kv_heads, d, _opts_ptr(opts), sm_count, ctypes.byref(plan)))
+    _check(load_library().attn_decode_query_plan(B, H, kv_heads, d, max_tokens, _opts_ptr(opts), sm_count, ctypes.byref(plan)))
     return plan
 
 

@@ -25,6 +25,20 @@ SAW_DECODE_HD int decode_tiles(int len, int tile) { return (int)(((unsigned)len 
 // Query heads of a block: the heads that share a K/V head in eights, 32 at most (8, 16 or 32).
 SAW_DECODE_HD int decode_rows(int group) { return group <= 8 ? 8 : group <= 16 ? 16 : 32; }
 
+// The form for short requests: a cluster of CTAs for each request and head block instead of even shares.  0: not that form.  It needs
+// all of them on the GPU at a time (`most` CTAs) and pays where even the longest request the tables can hold gives a CTA few tiles: up
+// to kDecodeFewTiles, or half as many again where the clusters fill half of the GPU and even shares would be hardly shorter.
+constexpr int kDecodeMaxCluster = 8;
+constexpr int kDecodeFewTiles = 4;
+SAW_DECODE_HD int decode_cluster(long long results, int max_len, int tile, int most) {
+    const int tiles = decode_tiles(max_len, tile);
+    int size = kDecodeMaxCluster;
+    while (size > 1 && (results * size > most || size / 2 >= tiles)) size /= 2;
+    if (results * size > most) return 0;
+    const int few = 2 * results * size > most ? kDecodeFewTiles * 3 / 2 : kDecodeFewTiles;
+    return tiles <= few * size ? size : 0;
+}
+
 // CTAs that get work, of a grid of `grid`.
 SAW_DECODE_HD int decode_ctas(uint64_t total, int grid) {
     const uint64_t most = (total + kDecodeMinTiles - 1) / kDecodeMinTiles;

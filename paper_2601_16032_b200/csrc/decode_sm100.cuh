@@ -37,6 +37,7 @@ struct DecodeParams {
     float2* part_ml;         // [2 grid][rows] reference (log2 units) and sum
     float* part_o;           // [2 grid][rows][d] sums
     float scale_log2;
+    int cluster;             // CTAs of a cluster in the form for short requests
     int B, H, kv_heads, group, head_blocks, max_len;
 };
 
@@ -102,8 +103,30 @@ struct DecodeCursor {
     }
 };
 
-// kN: warps of a group, and blocks of 8 query heads.
-template <int kD, int kBf16, int kN>
+__device__ __forceinline__ uint32_t in_cta(uint32_t smem_addr, int rank)       // the same place in another CTA of the cluster
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t a)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// kN: warps of a group, and blocks of 8 query heads.  kCluster: the form for short requests (decode_cluster): a cluster of CTAs has one
+// request and head block, each CTA an even part of its tiles, and they join their sums through each other's shared memory: no
+// scan over the lengths, nothing through global memory, no second launch.
+template <int kD, int kBf16, int kN, bool kCluster>
 __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const DecodeParams p)
 {
     using G = DecodeGeometry<kD>;
@@ -117,6 +140,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
     __shared__ uint64_t scan[kDecodeWarps];
     __shared__ int start_at;
     __shared__ uint64_t start_off;
+    __shared__ float2 cluster_ml[kCluster ? kRows : 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int group = warp / kN, member = warp % kN;
     const int blocks = p.kv_heads * p.head_blocks;
@@ -125,55 +149,76 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kN) : "memory");
     };
 
-    // ---- this CTA's share: sum of all requests' tiles, then the request and tile the share begins with
-    const int chunk = (p.B + kDecodeThreads - 1) / kDecodeThreads, b_lo = min(p.B, tid * chunk), b_hi = min(p.B, b_lo + chunk);
-    uint64_t mine = 0;
-    bool bad = false;
-    for (int b = b_lo; b < b_hi; ++b) {
-        const int raw = p.seq_len[b];
-        bad |= raw < 0 || raw > p.max_len;
-        mine += (uint64_t)decode_tiles(decode_cut(p, raw), G::kTile) * blocks;
-    }
-    if (bad && blockIdx.x == 0) note_index(p.status, kIndexLength);
-    uint64_t upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t u = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += u;
-    }
-    if (lane == 31) scan[warp] = upto;
-    __syncthreads();
-    uint64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < kDecodeWarps; ++w) {
-        if (w < warp) upto += scan[w];
-        total += scan[w];
-    }
-    const int ctas = decode_ctas(total, gridDim.x), cta = blockIdx.x;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int joins = 0;     // bit i: entry 2 cta + i of p.join is written
-    if (cta < ctas) {
-        const uint64_t begin = decode_share_begin(total, ctas, cta), end = decode_share_begin(total, ctas, cta + 1);
-        int left = (int)(end - begin);
-        if (begin >= upto - mine && begin < upto) {
-            uint64_t at = begin - (upto - mine);
-            int b = b_lo;
-            for (;; ++b) {
-                const uint64_t t = (uint64_t)decode_tiles(decode_cut(p, p.seq_len[b]), G::kTile) * blocks;
-                if (at < t) break;
-                at -= t;
-            }
-            start_at = b;
-            start_off = at;
-        }
-        __syncthreads();
-        DecodeCursor<G::kTile> ld;
-        ld.b = start_at;
-        ld.len = decode_cut(p, p.seq_len[ld.b]);
-        ld.next_raw = ld.b + 1 < p.B ? p.seq_len[ld.b + 1] : 0;
+    DecodeCursor<G::kTile> ld;
+    int left;                        // tiles of this CTA's share
+    int joins = 0;                   // bit i: entry 2 cta + i of p.join is written
+    const int cta = blockIdx.x;
+    uint64_t total = 0, end = 0;
+    int ctas = 0;
+    if (kCluster) {
+        const int result = cta / p.cluster, rank = cta % p.cluster;
+        ld.b = result / blocks;
+        ld.block = result % blocks;
+        const int raw = p.seq_len[ld.b];
+        if (cta % (blocks * p.cluster) == 0 && tid == 0 && (raw < 0 || raw > p.max_len)) note_index(p.status, kIndexLength);
+        ld.len = decode_cut(p, raw);
+        ld.next_raw = 0;
         ld.n = decode_tiles(ld.len, G::kTile);
-        ld.block = (int)decode_div(start_off, (uint64_t)ld.n);
-        ld.tile = (int)(start_off - (uint64_t)ld.block * (uint64_t)ld.n);
+        ld.tile = ld.n * rank / p.cluster;
+        left = ld.n * (rank + 1) / p.cluster - ld.tile;
+        if (tid < kRows) cluster_ml[tid] = make_float2(-INFINITY, 0.f);      // (stands if there are no tiles)
+    } else {
+        // ---- this CTA's share: sum of all requests' tiles, then the request and tile the share begins with
+        const int chunk = (p.B + kDecodeThreads - 1) / kDecodeThreads, b_lo = min(p.B, tid * chunk), b_hi = min(p.B, b_lo + chunk);
+        uint64_t mine = 0;
+        bool bad = false;
+        for (int b = b_lo; b < b_hi; ++b) {
+            const int raw = p.seq_len[b];
+            bad |= raw < 0 || raw > p.max_len;
+            mine += (uint64_t)decode_tiles(decode_cut(p, raw), G::kTile) * blocks;
+        }
+        if (bad && cta == 0) note_index(p.status, kIndexLength);
+        uint64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t u = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += u;
+        }
+        if (lane == 31) scan[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kDecodeWarps; ++w) {
+            if (w < warp) upto += scan[w];
+            total += scan[w];
+        }
+        ctas = decode_ctas(total, gridDim.x);
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        left = 0;
+        if (cta < ctas) {
+            const uint64_t begin = decode_share_begin(total, ctas, cta);
+            end = decode_share_begin(total, ctas, cta + 1);
+            left = (int)(end - begin);
+            if (begin >= upto - mine && begin < upto) {
+                uint64_t at = begin - (upto - mine);
+                int b = b_lo;
+                for (;; ++b) {
+                    const uint64_t t = (uint64_t)decode_tiles(decode_cut(p, p.seq_len[b]), G::kTile) * blocks;
+                    if (at < t) break;
+                    at -= t;
+                }
+                start_at = b;
+                start_off = at;
+            }
+            __syncthreads();
+            ld.b = start_at;
+            ld.len = decode_cut(p, p.seq_len[ld.b]);
+            ld.next_raw = ld.b + 1 < p.B ? p.seq_len[ld.b + 1] : 0;
+            ld.n = decode_tiles(ld.len, G::kTile);
+            ld.block = (int)decode_div(start_off, (uint64_t)ld.n);
+            ld.tile = (int)(start_off - (uint64_t)ld.block * (uint64_t)ld.n);
+        }
+    }
+    if (left > 0) {
         DecodeCursor<G::kTile> cp = ld;
         int to_load = left;
 
@@ -255,8 +300,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             }
         };
 
+        // (In the cluster form the last tile is to lie in stage 1, so that stage 0 is free for the sums.)
+        static_assert(!kCluster || kStages == 2, "the stage of the last tile");
+        int stage = kCluster ? left & 1 : 0;
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) issue(s);
+        for (int s = 0; s < kStages - 1; ++s) issue(stage + s);
         load_q();
         float acc[kD / 16][4];                // O^T: 16 dimensions x 8 heads a block; this lane's columns are heads 2 (lane & 3) and the next
         float ref[2], l[2];                   // of those heads: the reference of the exponents, and this lane's share of the sum
@@ -267,7 +315,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             for (int j = 0; j < kD / 16; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
         };
         clear();
-        int stage = 0, first_tile = cp.tile;
+        int first_tile = cp.tile;
         // ldmatrix: the row and piece that this lane gives the address of.  K as A operand (tokens x dimensions): blocks in the order tokens
         // 0-7 and 8-15, then the next 8 dimensions; V transposed (dimensions x tokens): dimensions 0-7 and 8-15, then the next 8 tokens.
         const int k_row = lane & 15, k_half = lane >> 4;
@@ -361,7 +409,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             if (ends || left == 1) {
                 // ---- the groups' sums meet in shared memory, each warp's in a part of the stage that its group has just emptied:
                 // [head][dimension], the dimension moved by 8 per pair of heads against bank conflicts
-                const bool starts = first_tile == 0, whole = starts && ends;
+                const bool starts = first_tile == 0, whole = !kCluster && starts && ends;
                 const int part = 2 * cta + (starts ? 1 : 0);
                 const int kvh = cp.block / p.head_blocks, first = (cp.block % p.head_blocks) * kRows;
                 const int rows = min(kRows, p.group - first);
@@ -404,7 +452,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
                         total_l += f * ml.y;
                     }
                     const int head = kvh * p.group + first + row;
-                    if (whole) {
+                    if (kCluster) {
+                        reinterpret_cast<float4*>(decode_smem)[row * (kD / 4) + piece] = sum;
+                        if (piece == 0) cluster_ml[row] = make_float2(big, total_l);
+                    } else if (whole) {
                         const float inv = 1.f / total_l;
                         *reinterpret_cast<uint2*>(p.o + (long long)done.b * p.o_request + (long long)head * p.o_head + 4 * piece) =
                             make_uint2(ptx::pack2<kBf16>(sum.x * inv, sum.y * inv), ptx::pack2<kBf16>(sum.z * inv, sum.w * inv));
@@ -415,7 +466,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
                     }
                 }
                 __syncthreads();   // the stages may be filled again
-                if (!whole && tid == 0) {
+                if (!kCluster && !whole && tid == 0) {
                     // Which CTAs hold the parts: those of the result's first and last tile.
                     const uint64_t now = end - (uint64_t)left;                   // this tile's place in the line
                     const int c0 = decode_cta_of(total, ctas, now - (uint64_t)done.tile), c1 = decode_cta_of(total, ctas, now + (uint64_t)(done.n - 1 - done.tile));
@@ -429,6 +480,49 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             stage = stage + 1 == kStages ? 0 : stage + 1;
         }
         cp_async_wait<0>();
+    }
+    if (kCluster) {
+        // ---- the cluster's sums: each CTA takes part of the rows and columns, and reads them from all
+        cluster_sync();
+        const int rank = cta % p.cluster, result = cta / p.cluster, b = result / blocks, block = result % blocks;
+        const int kvh = block / p.head_blocks, first = (block % p.head_blocks) * kRows, rows = min(kRows, p.group - first);
+        const uint32_t ml_at = ptx::smem_u32(cluster_ml), sums_at = ptx::smem_u32(decode_smem);
+#pragma unroll 2
+        for (int i = rank * kDecodeThreads + tid; i < rows * (kD / 4); i += p.cluster * kDecodeThreads) {
+            const int row = i / (kD / 4), piece = i % (kD / 4);
+            float2 ml[kDecodeMaxCluster];
+            float4 x[kDecodeMaxCluster];
+            float big = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < kDecodeMaxCluster; ++c) {       // all on their way together
+                ml[c] = make_float2(-INFINITY, 0.f);
+                x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c < p.cluster) {
+                    ml[c] = ld_cluster2(in_cta(ml_at + 8 * row, c));
+                    x[c] = ld_cluster4(in_cta(sums_at + 16 * i, c));
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kDecodeMaxCluster; ++c) {
+                if (ml[c].x == -INFINITY && ml[c].y == 0.f) x[c] = make_float4(0.f, 0.f, 0.f, 0.f);      // no tiles: whatever was there
+                big = fmaxf(big, ml[c].x);
+            }
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            float total_l = 0.f;
+#pragma unroll
+            for (int c = 0; c < kDecodeMaxCluster; ++c) {
+                const float f = ml[c].x == -INFINITY ? 1.f : ptx::ex2(ml[c].x - big);
+                sum.x += f * x[c].x; sum.y += f * x[c].y; sum.z += f * x[c].z; sum.w += f * x[c].w;
+                total_l += f * ml[c].y;
+            }
+            const float inv = ld.n == 0 ? 0.f : 1.f / total_l;        // no tokens: zeros
+            const int head = kvh * p.group + first + row;
+            *reinterpret_cast<uint2*>(p.o + (long long)b * p.o_request + (long long)head * p.o_head + 4 * piece) =
+                make_uint2(ptx::pack2<kBf16>(sum.x * inv, sum.y * inv), ptx::pack2<kBf16>(sum.z * inv, sum.w * inv));
+            if (p.lse && piece == 0) p.lse[(long long)b * p.H + head] = (big - kBias + log2f(total_l)) * 0.6931471805599453f;
+        }
+        cluster_sync();       // nobody leaves while its shared memory may be read
+        return;
     }
     if (tid == 0) {
         if (!(joins & 1)) p.join[2 * cta] = make_int4(0, 0, 0, 0);

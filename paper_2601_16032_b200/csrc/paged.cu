@@ -19,7 +19,7 @@ constexpr int kMaxPageSize = 65536;
 constexpr int kMaxHeads = 65536;
 constexpr int kRopeMaxCtas = 1024;     // of the backward pass; its workspace holds a partial sum of each
 
-enum RaisedBit { kRaisedPlan = 0, kRaisedDecode = 1 };
+enum RaisedBit { kRaisedPlan = 0, kRaisedDecode = 1 };   // kRaisedDecode .. + 23: the forms of the decode kernel
 
 // A rectangular region of memory: `outer` steps of `outer_stride`, each of `inner` steps of `inner_stride`, each of `bytes`.
 struct Region {
@@ -231,18 +231,25 @@ RopeKernel rope_kernel(int d, int dtype, int style, bool backward) {
 }
 
 using DecodeKernel = void (*)(const DecodeParams);
-template <int kD, int kBf16, int kN>
-int launch_decode_rows(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
-    constexpr int kSmem = DecodeGeometry<kD>::kSmem, kBit = kRaisedDecode + ((kD == 128) * 2 + kBf16) * 3 + kN / 2;
-    DecodeKernel kernel = decode_paged_kernel<kD, kBf16, kN>;
+template <int kD, int kBf16, int kN, bool kCluster>
+int launch_decode_form(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
+    constexpr int kSmem = DecodeGeometry<kD>::kSmem, kBit = kRaisedDecode + ((kD == 128) * 4 + kBf16 * 2 + kCluster) * 3 + kN / 2;
+    DecodeKernel kernel = decode_paged_kernel<kD, kBf16, kN, kCluster>;
     int rc = raise_smem(dev, ds, (const void*)kernel, kBit, kSmem);
-    return rc ? rc : launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, 0, false, p));
+    return rc ? rc : launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, kCluster ? p.cluster : 0, false, p));
+}
+template <int kD, int kBf16, bool kCluster>
+int launch_decode_rows(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
+    const int rows = decode_rows(p.group);
+    return rows == 8 ? launch_decode_form<kD, kBf16, 1, kCluster>(dev, ds, p, grid, st) : rows == 16 ? launch_decode_form<kD, kBf16, 2, kCluster>(dev, ds, p, grid, st)
+                                                                                         : launch_decode_form<kD, kBf16, 4, kCluster>(dev, ds, p, grid, st);
 }
 template <int kD, int kBf16>
-int launch_decode(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
-    const int rows = decode_rows(p.group);
-    int rc = rows == 8 ? launch_decode_rows<kD, kBf16, 1>(dev, ds, p, grid, st) : rows == 16 ? launch_decode_rows<kD, kBf16, 2>(dev, ds, p, grid, st)
-                                                                                : launch_decode_rows<kD, kBf16, 4>(dev, ds, p, grid, st);
+int launch_decode(int dev, const DeviceState& ds, DecodeParams& p, int grid, cudaStream_t st) {
+    const long long results = (long long)p.B * p.kv_heads * p.head_blocks;
+    p.cluster = decode_cluster(results, p.max_len, decode_tile(kD), grid);
+    if (p.cluster) return launch_decode_rows<kD, kBf16, true>(dev, ds, p, (int)(results * p.cluster), st);
+    int rc = launch_decode_rows<kD, kBf16, false>(dev, ds, p, grid, st);
     return rc ? rc : launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, 1, kJoinThreads, 0, st, 0, true, p));
 }
 
@@ -413,13 +420,13 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
     rope_kernel(d, dtype, rot_style, true)<<<grid, kRopeThreads, 0, st>>>(p);
     if ((rc = launch_status(cudaGetLastError()))) return rc;
     if (dq_weight || dk_weight) {
-        rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 32, 1, 1024, 0, st, 0, true, (const float*)p.partial, grid, d, dq_weight, dk_weight));
+        rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 8, 1, 1024, 0, st, 0, true, (const float*)p.partial, grid, d, dq_weight, dk_weight));
         if (rc) return rc;
     }
     return z.check_mode ? read_status(nullptr) : ATTN_OK;
 }
 
-int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_opts* opts, int sm_count, attn_decode_plan* out) {
+int attn_decode_query_plan(int B, int H, int kv_heads, int d, long long max_tokens, const attn_decode_opts* opts, int sm_count, attn_decode_plan* out) {
     if (!out) return fail(ATTN_ERR_INVALID_ARG, "out is null");
     attn_decode_opts z;
     memset(&z, 0, sizeof(z));
@@ -438,6 +445,8 @@ int attn_decode_query_plan(int B, int H, int kv_heads, int d, const attn_decode_
     const int rows = decode_rows(H / kv_heads);
     out->head_blocks = (H / kv_heads + rows - 1) / rows;
     out->min_tiles = kDecodeMinTiles;
+    if (max_tokens < 0) return fail(ATTN_ERR_INVALID_ARG, "max_tokens must not be negative");
+    out->cluster = max_tokens == 0 ? 0 : decode_cluster((long long)B * kv_heads * out->head_blocks, max_tokens < 2147483647ll ? (int)max_tokens : 2147483647, decode_tile(d), out->grid);
     out->workspace_bytes = decode_workspace(out->grid, rows, d);
     return ATTN_OK;
 }
@@ -447,7 +456,7 @@ int attn_decode_trace(const int* seq_len, int B, int H, int kv_heads, int d, con
     if (!n || !seq_len) return fail(ATTN_ERR_INVALID_ARG, "seq_len and n must be non-null");
     if (cap > 0 && !buf) return fail(ATTN_ERR_INVALID_ARG, "buf is null");
     attn_decode_plan plan;
-    int rc = attn_decode_query_plan(B, H, kv_heads, d, opts, sm_count, &plan);
+    int rc = attn_decode_query_plan(B, H, kv_heads, d, 0, opts, sm_count, &plan);
     if (rc) return rc;
     const int blocks = kv_heads * plan.head_blocks;
     uint64_t total = 0;

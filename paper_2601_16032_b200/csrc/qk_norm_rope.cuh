@@ -484,21 +484,30 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
     }
 }
 
-// dq_weight[c] and dk_weight[c] = the sum of the CTAs' partial sums, in their order: 32 columns a CTA, 32 threads a column.
+// dq_weight[c] and dk_weight[c] = the sum of the CTAs' partial sums in a fixed order: 8 columns a CTA, 128 threads a column, each with every
+// 128th CTA's, so that it takes two or three rounds of loads.
 __global__ void __launch_bounds__(1024) rope_weight_sum_kernel(const float* partial, int ctas, int d, float* dq_weight, float* dk_weight)
 {
-    __shared__ float sums[32][33];
+    __shared__ float sums[32][8];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int col = threadIdx.x & 31, row = threadIdx.x >> 5, column = blockIdx.x * 32 + col;   // of 2 d
+    const int col = threadIdx.x & 7, row = threadIdx.x >> 3, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, column = blockIdx.x * 8 + col;   // of 2 d
     float a = 0.f;
-    for (int c = row; c < ctas; c += 32) a += partial[(long long)c * 2 * d + column];
-    sums[row][col] = a;
+#pragma unroll 4
+    for (int c = row; c < ctas; c += 128) a += partial[(long long)c * 2 * d + column];
+    a += __shfl_xor_sync(0xffffffffu, a, 8);
+    a += __shfl_xor_sync(0xffffffffu, a, 16);
+    if (lane < 8) sums[warp][col] = a;
     __syncthreads();
-    if (row == 0) {
+    if (warp == 0) {
         float t = 0.f;
-        for (int r = 0; r < 32; ++r) t += sums[r][col];
-        float* out = column < d ? dq_weight : dk_weight;
-        if (out) out[column < d ? column : column - d] = t;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) t += sums[row * 8 + r][col];        // rows 0 to 3 here
+        t += __shfl_xor_sync(0xffffffffu, t, 8);
+        t += __shfl_xor_sync(0xffffffffu, t, 16);
+        if (lane < 8) {
+            float* out = column < d ? dq_weight : dk_weight;
+            if (out) out[column < d ? column : column - d] = t;
+        }
     }
 }
 

@@ -271,7 +271,7 @@ py::tuple decode_paged(const Tensor& q, const Tensor& k_cache, const Tensor& v_c
     size_t bytes = 0;
     if (!workspace_given) {
         attn_decode_plan plan;
-        check(attn_decode_query_plan((int)B, (int)H, cache.kv_heads, (int)d, &opts, 0, &plan));
+        check(attn_decode_query_plan((int)B, (int)H, cache.kv_heads, (int)d, 0, &opts, 0, &plan));
         bytes = plan.workspace_bytes;
     }
     Tensor workspace = workspace_of(workspace_given, bytes, q);

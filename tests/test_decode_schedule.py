@@ -17,7 +17,8 @@ def built():
 def check(lengths, H, kv_heads, d, max_ctas=0, sm_count=148):
     o = sa.DecodeOpts()
     o.max_ctas = max_ctas
-    plan = sa.attn_decode_query_plan(len(lengths), H, kv_heads, d, o, sm_count)
+    plan = sa.attn_decode_query_plan(len(lengths), H, kv_heads, d, 0, o, sm_count)
+    assert plan.cluster == 0
     group = H // kv_heads
     assert plan.head_blocks == -(-group // 32) and plan.grid <= (max_ctas or 3 * sm_count)
     assert plan.workspace_bytes >= plan.grid * 2 * min(group, 32) * (d + 2) * 4
@@ -78,3 +79,21 @@ def test_plan_refusals():
         assert e.value.status == status
     with pytest.raises(sa.AttnError):
         sa.attn_decode_trace([-1], 4, 2, 128, sm_count=148)
+
+
+def test_clusters_for_short_requests():
+    """All CTAs fit on the GPU at a time, no CTA has more than a handful of tiles, and a cluster is no larger than there are tiles for."""
+    plan = lambda B, kv_heads, d, tokens, **o: sa.attn_decode_query_plan(B, 4 * kv_heads, kv_heads, d, tokens, sa.DecodeOpts(**o), 148)  # noqa: E731
+    assert plan(1, 8, 128, 1008).cluster == 8 and plan(1, 8, 128, 131072).cluster == 0 and plan(64, 8, 128, 1008).cluster == 0
+    assert plan(1, 8, 128, 64).cluster == 1 and plan(1, 8, 128, 65).cluster == 2 and plan(1, 8, 128, 0).cluster == 0
+    assert plan(1, 8, 128, 1008, max_ctas=63).cluster == 4 and plan(1, 8, 128, 1008, max_ctas=7).cluster == 0
+    for B in (1, 2, 7, 30, 100, 444, 445, 3000):
+        for kv_heads in (1, 3, 8):
+            for d in (64, 128):
+                for tokens in (1, 64, 128, 129, 700, 2048, 2049, 4096, 5000, 1 << 40):
+                    p = plan(B, kv_heads, d, tokens)
+                    if p.cluster:
+                        tiles = -(-tokens // p.tile_tokens)
+                        assert p.cluster in (1, 2, 4, 8) and B * kv_heads * p.cluster <= p.grid and -(-tiles // p.cluster) <= 6
+    with pytest.raises(sa.AttnError):
+        plan(1, 1, 128, -1)
