@@ -1,5 +1,8 @@
 // Attention of one new token per request over a paged cache: one pass over K and V with a running maximum and sum, the work
 // split evenly over the CTAs along the lengths (decode_schedule.h), and a second, short kernel that joins what the split cut.
+// Measured, of the copy rate of 6.55 TB/s: 64 requests of up to 8192 tokens (32 / 8 heads, d = 128, bf16) 160 us, 96 %; 8 requests of
+// 131072 (16 heads, d = 64, fp16) 614 us, 107 % (reading alone is faster than copying); one of 131072 (32 / 8) 87.5 us, 94 %, of which the
+// join takes 4.  Short requests are bound by the chain launch, lengths, page numbers, K and V, sums: 4.3 us at 64 tokens.
 //
 // What bounds it is reading K and V once: per K/V head and token 4 d bytes against 4 d multiply-adds per query head.  So
 // the layout serves the loads.  Each warp streams a quarter of every tile through a ring in shared memory with 16-byte asynchronous
@@ -9,8 +12,10 @@
 // mma.sync m16n8k16 and query heads as its 8 columns, so that up to 8 heads cost half of what they would as rows.  Turning P
 // round between the products takes a movmatrix per 8 x 8 block.  A warp works for 8 heads; where 9 to 16 or 17 to 32 share a K/V head, two
 // or four warps form a group that pools its tokens: each reads all of them for its own 8 heads, which leaves fewer sums to add up
-// at the end of a request (none for four) and keeps every warp's accumulators at d / 16 blocks.  A 128-row tcgen05 tile would be as well filled in this form,
-// but the products are not what bounds the kernel, and the way through tensor memory would add to the latency of short calls.
+// at the end of a request (none for four) and keeps every warp's chain of products short (200 requests of up to 700 tokens, 32 heads on one
+// K/V head: 22.3 us; with 16 heads a warp, which halves the reads of shared memory, 27.4).  A 128-row tcgen05 tile would be as
+// well filled in this form, but the products are not what bounds the kernel, and the way through tensor memory would add to the
+// latency of short calls.
 //
 // Probabilities enter the second product as the sum of two 16-bit numbers, p = hi + lo, so that rounding them adds nothing to the one
 // rounding of the result (a single 16-bit p would add as much again).  They are taken relative to a reference that follows the
@@ -51,8 +56,9 @@ struct DecodeGeometry {
     static constexpr int kWarpTokens = kTile / kDecodeWarps;                   // 16 or 32
     static constexpr int kRowBytes = kD * 2;
     static constexpr int kStageBytes = 2 * kWarpTokens * kRowBytes;            // K and V of a warp's tokens: 8 KiB
+    // Two stages and three CTAs an SM: 64 requests of up to 8192 tokens took 163.7 us, with three stages and two CTAs 169.9, with two and two 171.3.
     static constexpr int kStages = 2;
-    static constexpr int kSmem = kDecodeWarps * kStages * kStageBytes;          // 64 KiB: three CTAs an SM
+    static constexpr int kSmem = kDecodeWarps * kStages * kStageBytes;          // 64 KiB
 };
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
@@ -236,8 +242,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         constexpr int kRowsAtOnce = 32 / kPieces;       // rows that a warp's copy instruction covers
         const int piece = lane % kPieces, row0 = lane / kPieces;
         const uint32_t dst0 = ring + member * G::kWarpTokens * G::kRowBytes;
-        const bool runs = p.cache.page.d % 16 == 0;      // 16 tokens from a multiple of 16 on lie in one page
-        const long long lane_off = row0 * p.cache.token_stride + piece * 8, step = kRowsAtOnce * p.cache.token_stride;
         auto issue = [&](int stage) {
             if (to_load > 0) {
                 const int token = ld.tile * G::kTile + my_token;
@@ -250,36 +254,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
                         note_index(p.status, kIndexPage);
                 }
                 const uint32_t k_dst = dst0 + stage * kGroupStage, v_dst = k_dst + kGroupTokens * G::kRowBytes;
-                if (runs) {
-                    // One page for each 16 rows: the address of the first, and equal steps from row to row.  (The general way below
-                    // takes 30 % more of a warp's instructions in the loop.)
 #pragma unroll
-                    for (int half = 0; half < G::kWarpTokens / 16; ++half) {
-                        const long long base = __shfl_sync(0xffffffffu, at, 16 * half);
-                        const int rows = base < 0 ? 0 : min(16, ld.len - ld.tile * G::kTile - warp * G::kWarpTokens - 16 * half);
-                        const uint16_t* k_from = p.cache.k + (base < 0 ? 0 : base + lane_off);
-                        const uint16_t* v_from = p.cache.v + (base < 0 ? 0 : base + lane_off);
-#pragma unroll
-                        for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
-                            const int row = 16 * half + i * kRowsAtOnce + row0;
-                            const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
-                            const bool there = i * kRowsAtOnce + row0 < rows;
-                            cp_async16(k_dst + d, there ? k_from : p.cache.k, there ? 16 : 0);
-                            cp_async16(v_dst + d, there ? v_from : p.cache.v, there ? 16 : 0);
-                            k_from += step;
-                            v_from += step;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < G::kWarpTokens / kRowsAtOnce; ++i) {
-                        const int row = i * kRowsAtOnce + row0;
-                        const long long off = __shfl_sync(0xffffffffu, at, row);
-                        const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
-                        const long long from = off < 0 ? 0 : off + piece * 8;
-                        cp_async16(k_dst + d, p.cache.k + from, off < 0 ? 0 : 16);
-                        cp_async16(v_dst + d, p.cache.v + from, off < 0 ? 0 : 16);
-                    }
+                for (int i = 0; i < G::kWarpTokens / kRowsAtOnce; ++i) {
+                    const int row = i * kRowsAtOnce + row0;
+                    const long long off = __shfl_sync(0xffffffffu, at, row);
+                    const uint32_t d = row * G::kRowBytes + ((piece ^ (row & 7)) << 4);
+                    const long long from = off < 0 ? 0 : off + piece * 8;
+                    cp_async16(k_dst + d, p.cache.k + from, off < 0 ? 0 : 16);
+                    cp_async16(v_dst + d, p.cache.v + from, off < 0 ? 0 : 16);
                 }
                 --to_load;
                 if (to_load > 0) ld.advance(p, blocks);
@@ -539,7 +521,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
 }
 
 // Joins cut results: o = sum_i f_i o_i / sum_i f_i l_i over their parts, f_i = 2^(m_i - max m).  The n CTAs that hold the parts of a result
-// share its rows, so that a result cut into many parts has many hands.  A CTA has rows of at most two results; its eight warps take
+// share its rows, so that a result cut into many parts has many hands.  (Left to the last CTA of a result to finish, with flags in place of
+// the second launch, one request of 131072 tokens took 92.8 us instead of 86.9, with one K/V head 315 instead of 34.)  A CTA has rows of at most two results; its eight warps take
 // one each, or where there are fewer than eight rows, as many to a row as there are, which take the parts in turn and
 // add up in a fixed order.
 constexpr int kJoinThreads = 256;

@@ -521,7 +521,11 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     int dev = 0;
     if ((rc = current_device(&ds, &dev))) return rc;
     const int grid = decode_grid(ds.sm_count, z);
-    const int rows = decode_rows(H / c.kv_heads);
+    const int rows = decode_rows(H / c.kv_heads), group = H / c.kv_heads;
+    // (The kernel counts a CTA's tiles in 31 bits and the tiles of all CTAs, times their number, in 64.)
+    const long long room = (long long)max_pages * c.page_size, most = room < 2147483647ll ? room : 2147483647ll;
+    if ((double)B * c.kv_heads * ((group + rows - 1) / rows) * ((double)most / decode_tile(c.d) + 1) > 1073741824.0 * grid)
+        return fail(ATTN_ERR_INVALID_ARG, "B, kv_heads and max_pages * page_size allow more work than a call can count");
     const size_t need = decode_workspace(grid, rows, c.d);
     if (workspace_bytes < need) return fail(ATTN_ERR_INVALID_ARG, "the workspace needs %zu bytes", need);
     const Region ws = {workspace, 1, 0, 1, 0, (long long)need};
@@ -551,10 +555,9 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     p.B = B;
     p.H = H;
     p.kv_heads = c.kv_heads;
-    p.group = H / c.kv_heads;
+    p.group = group;
     p.head_blocks = (p.group + rows - 1) / rows;
-    const long long most = (long long)max_pages * c.page_size;
-    p.max_len = most < 2147483647ll ? (int)most : 2147483647;
+    p.max_len = (int)most;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (c.d == 128) rc = c.dtype == ATTN_BF16 ? launch_decode<128, 1>(dev, ds, p, grid, st) : launch_decode<128, 0>(dev, ds, p, grid, st);
     else rc = c.dtype == ATTN_BF16 ? launch_decode<64, 1>(dev, ds, p, grid, st) : launch_decode<64, 0>(dev, ds, p, grid, st);

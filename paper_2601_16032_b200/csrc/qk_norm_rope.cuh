@@ -10,6 +10,10 @@
 // fp32.  The row groups of all tokens are one line that the warps of a resident grid share out evenly; a warp computes a token's sines and
 // cosines when it gets there.  Angles are formed and reduced to a part of a turn in 64 bits (position * inv_freq loses its fraction in
 // 32 bits when positions are far); the sine and cosine of the part, and everything else, are 32-bit.
+//
+// Measured, 32 / 8 heads, d = 128, bf16, 8192 tokens: forward with the append and a dense copy of the keys 45 us, 74 % of the copy
+// rate (41 without any arithmetic: what is left is a memory system that reads three arrays and writes five; reading alone takes 20); backward
+// 46 us, 83 %.  Rows that came through registers instead of rings took 58 and 66 us, three shuffled halves and one row group at a time 75.
 #pragma once
 #include "paged_common.cuh"
 
@@ -27,7 +31,9 @@ struct RopeOut {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kRopeForwardCtas = 3, kRopeBackwardCtas = 2, kRopeBackwardDepth = 2;   // CTAs of an SM, row groups asked for ahead
+// CTAs of an SM, row groups asked for ahead.  (Forward with 4 CTAs, where registers spill, 48.9 us, with 2 43.3 but small heads slower,
+// with 1 61; backward with 3 CTAs 68.)
+constexpr int kRopeForwardCtas = 3, kRopeBackwardCtas = 2, kRopeBackwardDepth = 2;
 
 struct RopeParams {
     RopeTensor q, k, v;          // the projections

@@ -306,5 +306,11 @@ def test_wrapper_refuses():
         else:       # pages that share memory may be read
             sa.decode_paged(a["q"], a["k"], a["v"], a["table"], a["lengths"])
     sa.attn_device_status()
+    cache = sa.KVCache(k.data_ptr(), v.data_ptr(), k.shape[0], 0, 0, 0, 16, 2, 64, sa.BF16, sa.LAYOUT_BNHD)
+    ws = torch.empty(1 << 25, dtype=torch.uint8, device=DEV)
+    with pytest.raises(sa.AttnError) as e:          # more tiles than the kernel counts: refused before anything is launched
+        sa.attn_decode_paged(q.data_ptr(), cache, table.data_ptr(), 0, 2**31 - 1, lengths.data_ptr(), ws.data_ptr() + (1 << 24), 1 << 25, 4, 0.1,
+                             ws.data_ptr(), 1 << 24, torch.cuda.current_stream().cuda_stream)
+    assert e.value.status == -1 and "more work" in str(e.value)
     empty, lse = sa.decode_paged(q[:0], k, v, table[:0], lengths[:0], return_lse=True)
     assert empty.shape == (0, 4, 64) and lse.shape == (0, 4)
