@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             if (begin >= upto - mine && begin < upto) {
                 uint64_t at = begin - (upto - mine);
                 int b = b_lo;
-                for (;; ++b) {
+                for (; b < b_hi - 1; ++b) {
                     const uint64_t t = (uint64_t)decode_tiles(decode_cut(p, p.seq_len[b]), G::kTile) * blocks;
                     if (at < t) break;
                     at -= t;

@@ -511,7 +511,7 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     if ((rc = check_decode_shape(B, H, c.kv_heads, c.d, z))) return rc;
     if (!block_table || !seq_len) return fail(ATTN_ERR_INVALID_ARG, "block_table and seq_len must be non-null");
     if (max_pages < 1 || table_stride < 0 || !fits_address(table_stride, B)) return fail(ATTN_ERR_INVALID_ARG, "max_pages must be positive, table_stride not negative");
-    if (!std::isfinite(scale)) return fail(ATTN_ERR_INVALID_ARG, "scale must be finite");
+    if (!std::isfinite(scale * 1.4426950408889634f)) return fail(ATTN_ERR_INVALID_ARG, "scale must be finite, and so must scale * log2(e)");
     if (((uintptr_t)block_table | (uintptr_t)seq_len | (uintptr_t)z.lse) & 3u) return fail(ATTN_ERR_ALIGNMENT, "block_table, seq_len and lse must be 4-byte aligned");
     Region rq, ro;
     if ((rc = rows_of("q", q, z.q_request, z.q_head, B, H, c.d, false, &rq)) || (rc = rows_of("o", o, z.o_request, z.o_head, B, H, c.d, true, &ro))) return rc;

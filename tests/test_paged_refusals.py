@@ -114,7 +114,7 @@ def decode_call(cache=None, opts=None, **change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(q=0), -1), (dict(table=0), -1), (dict(lens=0), -1), (dict(o=0), -1), (dict(ws=0), -1), (dict(ws=at(4) + 8), -3), (dict(B=0), -1), (dict(H=7), -1),
-    (dict(H=0), -1), (dict(pages=0), -1), (dict(stride=-1), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(q=at(0) + 4), -3),
+    (dict(H=0), -1), (dict(pages=0), -1), (dict(stride=-1), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(scale=3e38), -1), (dict(q=at(0) + 4), -3),
     (dict(lens=at(2) + 2), -3), (dict(opts=dict(lse=at(5) + 2)), -3), (dict(opts=dict(max_ctas=-1)), -1), (dict(opts=dict(check_mode=2)), -1),
     (dict(opts=dict(q_head=4)), -1), (dict(opts=dict(o_request=64, o_head=128)), -1), (dict(cache=dict(d=80)), -2), (dict(cache=dict(k=0)), -1),
     (dict(cache=dict(v=at(14))), -1), (dict(cache=dict(page_size=0)), -1), (dict(cache=dict(kv_heads=3)), -1), (dict(cache=dict(dtype=4)), -1),
