@@ -109,26 +109,6 @@ struct DecodeCursor {
     }
 };
 
-__device__ __forceinline__ uint32_t in_cta(uint32_t smem_addr, int rank)       // the same place in another CTA of the cluster
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ float2 ld_cluster2(uint32_t a)
-{
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 ld_cluster4(uint32_t a)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // kN: warps of a group, and blocks of 8 query heads.  kCluster: the form for short requests (decode_cluster): a cluster of CTAs has one
 // request and head block, each CTA an even part of its tiles, and they join their sums through each other's shared memory: no
 // scan over the lengths, nothing through global memory, no second launch.
@@ -415,8 +395,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         mine_o[(2 * (lane & 3) + (c & 1)) * kD + ((16 * j + (lane >> 2) + 8 * (c >> 1)) ^ ((lane & 3) << 3))] = acc[j][c];
+                // (In the cluster form the sums of a single group are read from where they are.)
+                if (kCluster && kGroups == 1 && lane < 8) cluster_ml[8 * member + lane] = warp_ml[warp][lane];
                 __syncthreads();
-                for (int i = tid; i < rows * (kD / 4); i += kDecodeThreads) {
+                for (int i = tid; i < rows * (kD / 4) && !(kCluster && kGroups == 1); i += kDecodeThreads) {
                     const int row = i / (kD / 4), piece = i % (kD / 4), m = row >> 3, r = row & 7;
                     float big = -INFINITY;
 #pragma unroll
@@ -468,24 +450,24 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         cluster_sync();
         const int rank = cta % p.cluster, result = cta / p.cluster, b = result / blocks, block = result % blocks;
         const int kvh = block / p.head_blocks, first = (block % p.head_blocks) * kRows, rows = min(kRows, p.group - first);
-        const uint32_t ml_at = ptx::smem_u32(cluster_ml), sums_at = ptx::smem_u32(decode_smem);
+        constexpr bool kInStage = kGroups == 1;
+        const uint32_t ml_at = ptx::smem_u32(cluster_ml), sums_at = ptx::smem_u32(decode_smem) + (kInStage ? kN * G::kStageBytes : 0);
 #pragma unroll 2
         for (int i = rank * kDecodeThreads + tid; i < rows * (kD / 4); i += p.cluster * kDecodeThreads) {
             const int row = i / (kD / 4), piece = i % (kD / 4);
+            const uint32_t at = sums_at + 16 * (kInStage ? row * (kD / 4) + (piece ^ (((row >> 1) & 3) << 1)) : i);
             float2 ml[kDecodeMaxCluster];
             float4 x[kDecodeMaxCluster];
             float big = -INFINITY;
 #pragma unroll
             for (int c = 0; c < kDecodeMaxCluster; ++c) {       // all on their way together
-                ml[c] = make_float2(-INFINITY, 0.f);
-                x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (c < p.cluster) {
-                    ml[c] = ld_cluster2(in_cta(ml_at + 8 * row, c));
-                    x[c] = ld_cluster4(in_cta(sums_at + 16 * i, c));
-                }
+                if (c >= p.cluster) break;
+                ml[c] = ld_cluster2(in_cta(ml_at + 8 * row, c));
+                x[c] = ld_cluster4(in_cta(at, c));
             }
 #pragma unroll
             for (int c = 0; c < kDecodeMaxCluster; ++c) {
+                if (c >= p.cluster) break;
                 if (ml[c].x == -INFINITY && ml[c].y == 0.f) x[c] = make_float4(0.f, 0.f, 0.f, 0.f);      // no tiles: whatever was there
                 big = fmaxf(big, ml[c].x);
             }
@@ -493,6 +475,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
             float total_l = 0.f;
 #pragma unroll
             for (int c = 0; c < kDecodeMaxCluster; ++c) {
+                if (c >= p.cluster) break;
                 const float f = ml[c].x == -INFINITY ? 1.f : ptx::ex2(ml[c].x - big);
                 sum.x += f * x[c].x; sum.y += f * x[c].y; sum.z += f * x[c].z; sum.w += f * x[c].w;
                 total_l += f * ml[c].y;

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(1024) page_plan_kernel(const PagePlanParams p)
                     : (taken > stack || stack - taken > p.capacity) ? ATTN_PLAN_NO_PAGES : ATTN_PLAN_FITS;
     const bool fits = state == ATTN_PLAN_FITS;
     // From here on `cached` and `free_count` may be overwritten by their outputs: all CTAs have read them.
-    if (p.in_place) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (p.in_place) cluster_sync();
 
     const int me = rank * threads + tid;
     if (me == 0) {

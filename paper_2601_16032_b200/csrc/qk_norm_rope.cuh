@@ -46,7 +46,8 @@ struct RopeParams {
     const long long* slot;       // null: no cache
     CacheView cache;
     int cache_head;              // its head stride
-    float* partial;              // backward pass: [CTA][2][d] sums for the weights
+    float* partial;              // backward pass: [CTA][2][d] sums for the weights; null: the grid is one cluster, which adds them up itself
+    float *dq_weight, *dk_weight;   // (with partial null)
     int* status;
     float eps;
     int T, H, kv_heads, rot, weight_f32;
@@ -359,7 +360,8 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
 
 // Backward: dn = R^T dy, g = dn w; with s = sum x^2 and t = sum g x over the row (one pass of shuffles for both), r = 1 / sqrt(s / d + eps),
 // dx = r (g - x r^2 t / d), dw += dn x r.  A lane keeps the weight sums of its eight columns over all of its rows (some dozens) in
-// registers; a CTA adds its warps' in a fixed order and leaves the sum in `partial`.
+// registers; a CTA adds its warps' in a fixed order and leaves the sum in `partial`, for rope_weight_sum_kernel, or where the rows are so few that
+// one cluster of CTAs has them all, in its shared memory for the cluster to add up (one launch instead of two).
 template <int kD, int kBf16, int kAdjacent>
 __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_bwd_kernel(const RopeParams p)
 {
@@ -485,8 +487,21 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
         if (threadIdx.x < kD) {
             float a = 0.f;
             for (int g = 0; g < kRopeWarps * kRows; ++g) a += sums[g][threadIdx.x];
-            p.partial[((long long)blockIdx.x * 2 + which) * kD + threadIdx.x] = a;
+            if (p.partial) p.partial[((long long)blockIdx.x * 2 + which) * kD + threadIdx.x] = a;
+            else weights[which][threadIdx.x] = a;
         }
+    }
+    if (!p.partial) {
+        cluster_sync();
+        const int i = (int)(blockIdx.x * kRopeThreads + threadIdx.x);
+        if (i < 2 * kD) {
+            float a = 0.f;
+            const uint32_t at = ptx::smem_u32(&weights[0][0]) + 4 * i;
+            for (int c = 0; c < (int)gridDim.x; ++c) a += ld_cluster1(in_cta(at, c));
+            float* out = i < kD ? p.dq_weight : p.dk_weight;
+            if (out) out[i % kD] = a;
+        }
+        cluster_sync();       // nobody leaves while its shared memory may be read
     }
 }
 

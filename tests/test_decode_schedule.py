@@ -86,7 +86,7 @@ def test_clusters_for_short_requests():
     plan = lambda B, kv_heads, d, tokens, **o: sa.attn_decode_query_plan(B, 4 * kv_heads, kv_heads, d, tokens, sa.DecodeOpts(**o), 148)  # noqa: E731
     assert plan(1, 8, 128, 1008).cluster == 8 and plan(1, 8, 128, 131072).cluster == 0 and plan(64, 8, 128, 1008).cluster == 0
     assert plan(1, 8, 128, 64).cluster == 1 and plan(1, 8, 128, 65).cluster == 2 and plan(1, 8, 128, 0).cluster == 0
-    assert plan(1, 8, 128, 1008, max_ctas=63).cluster == 4 and plan(1, 8, 128, 1008, max_ctas=7).cluster == 0
+    assert plan(1, 8, 128, 1008, max_ctas=63).cluster == 4 and plan(1, 8, 128, 1008, max_ctas=7).cluster == 0 and plan(112, 8, 128, 60).cluster == 0 and plan(111, 8, 128, 60).cluster == 1
     for B in (1, 2, 7, 30, 100, 444, 445, 3000):
         for kv_heads in (1, 3, 8):
             for d in (64, 128):
@@ -94,6 +94,7 @@ def test_clusters_for_short_requests():
                     p = plan(B, kv_heads, d, tokens)
                     if p.cluster:
                         tiles = -(-tokens // p.tile_tokens)
-                        assert p.cluster in (1, 2, 4, 8) and B * kv_heads * p.cluster <= p.grid and -(-tiles // p.cluster) <= 6
+                        assert p.cluster in (1, 2, 4, 8) and -(-tiles // p.cluster) <= 6
+                        assert B * kv_heads * p.cluster <= p.grid or (p.cluster == 1 and B * kv_heads <= 2 * p.grid)
     with pytest.raises(sa.AttnError):
         plan(1, 1, 128, -1)
