@@ -508,9 +508,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
 // the second launch, one request of 131072 tokens took 92.8 us instead of 86.9, with one K/V head 315 instead of 34.)  A CTA has rows of at most two results; its eight warps take
 // one each, or where there are fewer than eight rows, as many to a row as there are, which take the parts in turn and
 // add up in a fixed order.
+// (Three CTAs' worth of registers, so that one fits where one of the decode's CTAs has ended: 64 requests of up to 500 tokens 21.0 us, with as
+// many as it likes 22.3.  Eight parts at a time where there are many: one request of 131072 tokens with one K/V head 25.4 us, four 30.4.)
 constexpr int kJoinThreads = 256;
+template <int kN>
+struct DecodeAhead { static constexpr int value = kN; };
 template <int kD, int kBf16>
-__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeParams p)
+__global__ void __launch_bounds__(kJoinThreads, 3) decode_join_kernel(const DecodeParams p)
 {
     constexpr int kWarps = kJoinThreads / 32, kCols = kD / 32;     // columns a lane sums
     constexpr float kBias = kBf16 ? 0.f : 7.f;
@@ -534,10 +538,10 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeP
         const int4 join = item < rows0 ? joins[0] : joins[1];
         const int n = there ? join.x : 0, c0 = join.y, row = cta - c0 + (item < rows0 ? item : item - rows0) * n;
         auto entry = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * block_rows + row; };
-        // Running reference, sum and columns over this warp's parts, kAhead of them read at a time.
-        constexpr int kAhead = 4;
+        // Running reference, sum and columns over this warp's parts: eight of them read at a time, the last few two at a time.
         float big = -INFINITY, acc[kCols] = {}, l = 0.f;
-        for (int i0 = lot; i0 < n; i0 += kAhead * to_a_row) {
+        auto take = [&](auto ahead, int i0) {
+            constexpr int kAhead = decltype(ahead)::value;
             float2 ml[kAhead];
             float x[kAhead][kCols];
 #pragma unroll
@@ -573,7 +577,12 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeP
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) acc[c] += f * x[a][c];
             }
-        }
+        };
+        int i0 = lot;
+#pragma unroll 1
+        for (; i0 + 4 * to_a_row < n; i0 += 8 * to_a_row) take(DecodeAhead<8>(), i0);
+#pragma unroll 1
+        for (; i0 < n; i0 += 2 * to_a_row) take(DecodeAhead<2>(), i0);
         if (to_a_row > 1) {
 #pragma unroll
             for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = acc[c];
