@@ -168,54 +168,89 @@ __device__ __forceinline__ float row_sum(float x)
 constexpr int kRopeDepth = 4;
 constexpr int kRopeTwice = 2;     // a row group is this many times as many rows as a warp holds at a time: the bookkeeping is shared by two
 
-struct RopeSegment {        // row groups of one token and kind that this warp takes
-    int token, kind, first, rows_left, n;      // first: this lane's first head; rows_left: of its rows, kRows apart
+// What differs from kind to kind (queries, keys, values), in shared memory: a warp changes kind every few row groups.
+struct __align__(16) RopeKind {
+    const uint16_t* src;     // the rows; second: of the backward pass, their gradients
+    const uint16_t* second;
+    uint16_t* out;           // queries' and keys' results (null for values, and for keys that go to the cache only)
+    uint16_t* cache;         // null for queries
+    int src_token, src_head, second_token, second_head, out_token, out_head, heads, groups;
 };
-template <int kRows>
-__device__ __forceinline__ RopeSegment rope_segment(const RopeParams& p, int token, int g, int left, int row)
+
+__device__ __forceinline__ void rope_stage_kinds(const RopeParams& p, RopeKind (&kinds)[3])
 {
-    const int kind = g < p.q_groups ? 0 : g < p.q_groups + p.k_groups ? 1 : 2;
-    const int from = g - (kind == 0 ? 0 : kind == 1 ? p.q_groups : p.q_groups + p.k_groups), here = kind == 0 ? p.q_groups : p.k_groups;
-    const int n = left < here - from ? left : here - from, first = from * kRows * kRopeTwice + row;
-    const int heads = (kind == 0 ? p.H : p.kv_heads) - first, mine = n * kRows * kRopeTwice - row;
-    return {token, kind, first, heads < mine ? heads : mine, n};
+    if (threadIdx.x == 0) {
+        kinds[0] = {p.q.p, p.dq_out.p, p.q_out.p, nullptr, p.q.token, p.q.head, p.dq_out.token, p.dq_out.head, p.q_out.token, p.q_out.head, p.H, p.q_groups};
+        kinds[1] = {p.k.p, p.dk_out.p, p.k_out.p, const_cast<uint16_t*>(p.cache.k), p.k.token, p.k.head, p.dk_out.token, p.dk_out.head, p.k_out.token, p.k_out.head,
+                    p.kv_heads, p.k_groups};
+        kinds[2] = {p.v.p, nullptr, nullptr, const_cast<uint16_t*>(p.cache.v), p.v.token, p.v.head, 0, 0, 0, 0, p.kv_heads, p.k_groups};
+    }
+    __syncthreads();
 }
 
+// A place in the line of row groups: group `from` of `kind` of a token.
+struct RopePlace {
+    int token, kind, from;
+    __device__ __forceinline__ RopePlace(const RopeParams& p, long long at) {
+        token = (int)rope_div(at, p.groups);
+        from = (int)(at - (long long)token * p.groups);
+        kind = 0;
+        if (from >= p.q_groups) { from -= p.q_groups; kind = 1; }
+        if (kind == 1 && from >= p.k_groups) { from -= p.k_groups; kind = 2; }
+    }
+    // Behind the n groups of this kind that a share has, the next kind begins.
+    __device__ __forceinline__ void next(int kinds) {
+        from = 0;
+        if (++kind == kinds) { kind = 0; ++token; }
+    }
+};
+
+// Row groups of one token and kind that a warp takes: how many, this lane's first head, and how many heads are left for it, kRows apart.
+template <int kRows>
+__device__ __forceinline__ void rope_segment(const RopeKind& kind, int from, int left, int row, int& n, int& first, int& rows_left)
+{
+    n = min(left, kind.groups - from);
+    first = from * (kRows * kRopeTwice) + row;
+    rows_left = min(kind.heads - first, n * (kRows * kRopeTwice) - row);
+}
+
+// The place that the copies have reached.
 template <int kRows, int kStreams>
 struct RopeStream {
-    RopeSegment seg;
+    RopePlace at;
     const uint16_t* src[kStreams];
     int half[kStreams];                 // elements from a row to the one kRows heads on
-    int left;                           // row groups of the share not asked for yet
-    int token, g, row, lane_col;
-    __device__ __forceinline__ void open(const RopeParams& p) {
-        seg = rope_segment<kRows>(p, token, g, left, row);
-        g += seg.n;
-        if (g == p.groups) { g = 0; ++token; }
-#pragma unroll
-        for (int s = 0; s < kStreams; ++s) {
-            const uint16_t* base = seg.kind == 0 ? (s ? p.dq_out.p : p.q.p) : seg.kind == 1 ? (s ? p.dk_out.p : p.k.p) : p.v.p;
-            const int by_token = seg.kind == 0 ? (s ? p.dq_out.token : p.q.token) : seg.kind == 1 ? (s ? p.dk_out.token : p.k.token) : p.v.token;
-            const int by_head = seg.kind == 0 ? (s ? p.dq_out.head : p.q.head) : seg.kind == 1 ? (s ? p.dk_out.head : p.k.head) : p.v.head;
-            src[s] = base + (long long)seg.token * by_token + (long long)seg.first * by_head + lane_col;
-            half[s] = by_head * kRows;
+    int left, n, rows_left;             // row groups of the share, and of the kind, not asked for yet
+    int row, lane_col, kinds;
+    __device__ __forceinline__ RopeStream(const RopePlace& start, int mine, int row_, int col, int kinds_)
+        : at(start), left(mine), n(0), rows_left(0), row(row_), lane_col(col), kinds(kinds_) {}
+    __device__ __forceinline__ void open(const RopeKind* table) {
+        const RopeKind& kind = table[at.kind];
+        int first;
+        rope_segment<kRows>(kind, at.from, left, row, n, first, rows_left);
+        src[0] = kind.src + (long long)at.token * kind.src_token + (long long)first * kind.src_head + lane_col;
+        half[0] = kind.src_head * kRows;
+        if (kStreams == 2) {
+            src[kStreams - 1] = kind.second + (long long)at.token * kind.second_token + (long long)first * kind.second_head + lane_col;
+            half[kStreams - 1] = kind.second_head * kRows;
         }
+        at.next(kinds);
     }
     // Asks for the next row group (or nothing, behind the last) into `slot`.
-    __device__ __forceinline__ void ask(const RopeParams& p, uint32_t slot) {
+    __device__ __forceinline__ void ask(const RopeParams& p, const RopeKind* table, uint32_t slot) {
         if (left > 0) {
-            if (seg.n == 0) open(p);
+            if (n == 0) open(table);
 #pragma unroll
             for (int s = 0; s < kStreams; ++s) {
 #pragma unroll
                 for (int h = 0; h < kRopeTwice; ++h) {
-                    const bool there = seg.rows_left > h * kRows;
+                    const bool there = rows_left > h * kRows;
                     cp_async16(slot + 512 * (kRopeTwice * s + h), there ? src[s] + h * half[s] : p.q.p, there ? 16 : 0);
                 }
                 src[s] += kRopeTwice * half[s];
             }
-            seg.rows_left -= kRows * kRopeTwice;
-            --seg.n;
+            rows_left -= kRows * kRopeTwice;
+            --n;
             --left;
         }
         cp_async_commit();
@@ -244,57 +279,51 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
     __shared__ __align__(16) float weights[2][kD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
     const RopeColumns<kAdjacent> col(p.rot, part);
+    __shared__ RopeKind table[3];
+    rope_stage_kinds(p, table);
     long long begin, end;
     rope_share(p, begin, end);
-    RopeStream<kRows, 1> stream;
-    const int mine = (int)(end - begin);
-    stream.left = mine;
-    stream.token = (int)rope_div(begin, p.groups);
-    stream.g = (int)(begin - (long long)stream.token * p.groups);
-    stream.row = row;
-    stream.lane_col = 8 * part;
-    stream.seg.n = 0;
-    int token = stream.token, g = stream.g;
+    const int mine = (int)(end - begin), kinds = p.slot ? 3 : 2;
+    RopePlace at(p, begin);
+    RopeStream<kRows, 1> stream(at, mine, row, 8 * part, kinds);
     const uint32_t ring = ptx::smem_u32(rings[warp]) + 16 * lane;       // a row group as it lies in memory: rows of kLanes pieces
 #pragma unroll 1
-    for (int i = 0; i < kRopeDepth; ++i) stream.ask(p, ring + 512 * kRopeTwice * i);
+    for (int i = 0; i < kRopeDepth; ++i) stream.ask(p, table, ring + 512 * kRopeTwice * i);
     rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     int slot = 0, have_token = -1;
     long long cache_at = -1;             // element offset of the token's first cache row; -1: none, -2: leave the token alone
 #pragma unroll 1
     for (int left = mine; left > 0;) {
-        RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
-        left -= seg.n;
-        if (token != have_token) {
-            have_token = token;
+        const RopeKind& kind = table[at.kind];
+        int n, first, rows_left;
+        rope_segment<kRows>(kind, at.from, left, row, n, first, rows_left);
+        left -= n;
+        if (at.token != have_token) {
+            have_token = at.token;
             cache_at = -1;
             if (p.slot) {
-                const long long at = p.slot[token];
-                if (at < 0) {
+                const long long slot_of = p.slot[at.token];
+                if (slot_of < 0) {
                     cache_at = -2;
                 } else {
-                    const long long page = at < 2147483648ll ? (long long)p.cache.page.div((uint32_t)at) : at / p.cache.page.d;
+                    const long long page = slot_of < 2147483648ll ? (long long)p.cache.page.div((uint32_t)slot_of) : slot_of / p.cache.page.d;
                     if (page >= p.cache.num_pages) note_index(p.status, kIndexSlot);
-                    else cache_at = page * p.cache.page_stride + (at - page * p.cache.page.d) * p.cache.token_stride;
+                    else cache_at = page * p.cache.page_stride + (slot_of - page * p.cache.page.d) * p.cache.token_stride;
                 }
             }
-            if (seg.kind != 2) rope_angles(p, token, turns[warp]);
+            if (at.kind != 2) rope_angles(p, at.token, turns[warp]);
         }
-        g += seg.n;
-        if (g == p.groups) { g = 0; ++token; }
         // Where the rows go: queries to q_out, keys to k_out, to the cache or to both, values to the cache.
-        const bool is_q = seg.kind == 0, is_v = seg.kind == 2, dense = is_q || (!is_v && p.k_out.p != nullptr);
+        const bool is_q = at.kind == 0, is_v = at.kind == 2, dense = kind.out != nullptr;
         const bool to_out = dense ? cache_at != -2 : cache_at >= 0;
         const bool to_both = dense && !is_q && cache_at >= 0;
-        uint16_t* cache = const_cast<uint16_t*>(is_v ? p.cache.v : p.cache.k) + cache_at + (long long)seg.first * p.cache_head + (is_v ? 8 * part : col.c0);
-        const int cache_half = p.cache_head * kRows;
-        const int out_head = is_q ? p.q_out.head : p.k_out.head, out_half = dense ? out_head * kRows : cache_half;
-        uint16_t* out = dense ? (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head + col.c0
-                              : cache;
+        uint16_t* cache = kind.cache + cache_at + (long long)first * p.cache_head + (is_v ? 8 * part : col.c0);
+        const int cache_half = p.cache_head * kRows, out_half = dense ? kind.out_head * kRows : cache_half;
+        uint16_t* out = dense ? kind.out + (long long)at.token * kind.out_token + (long long)first * kind.out_head + col.c0 : cache;
         const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
         ptx::f32x2 uc[2], vs[2], vc[2], us[2];        // wu cos, -wv sin, wv cos, wu sin
         if (!is_v) {
-            const float4 wu = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part]), wv = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part + 4]);
+            const float4 wu = *reinterpret_cast<const float4*>(&weights[at.kind][8 * part]), wv = *reinterpret_cast<const float4*>(&weights[at.kind][8 * part + 4]);
             float4 t0 = make_float4(1.f, 0.f, 1.f, 0.f), t1 = t0;      // cos, sin, cos, sin
             if (col.turns) {
                 t0 = *reinterpret_cast<const float4*>(&turns[warp][4 * part]);
@@ -306,7 +335,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
             vs[0] = ptx::pack_f32x2(-wv.x * t0.y, -wv.y * t0.w); vs[1] = ptx::pack_f32x2(-wv.z * t1.y, -wv.w * t1.w);
         }
 #pragma unroll 1
-        for (int i = 0; i < seg.n; ++i) {
+        for (int i = 0; i < n; ++i) {
             cp_async_wait<kRopeDepth - 1>();
             __syncwarp();
             uint4 x[kRopeTwice];
@@ -315,7 +344,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
                 x[h] = is_v ? *reinterpret_cast<const uint4*>(&rings[warp][slot][512 * h + 16 * lane])
                             : col.load(reinterpret_cast<const uint16_t*>(&rings[warp][slot][512 * h + 2 * kD * row]));
             __syncwarp();
-            stream.ask(p, ring + 512 * kRopeTwice * slot);
+            stream.ask(p, table, ring + 512 * kRopeTwice * slot);
             slot = slot + 1 == kRopeDepth ? 0 : slot + 1;
             if (!is_v) {
 #pragma unroll
@@ -343,7 +372,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
             if (to_out) {
 #pragma unroll
                 for (int h = 0; h < kRopeTwice; ++h) {
-                    if (seg.rows_left > h * kRows) {
+                    if (rows_left > h * kRows) {
                         if (is_v) *reinterpret_cast<uint4*>(out + h * out_half) = x[h];
                         else col.store_at(out + h * out_half, x[h]);
                         if (to_both) col.store_at(cache + h * cache_half, x[h]);
@@ -352,8 +381,9 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
             }
             out += kRopeTwice * out_half;
             cache += kRopeTwice * cache_half;
-            seg.rows_left -= kRows * kRopeTwice;
+            rows_left -= kRows * kRopeTwice;
         }
+        at.next(kinds);
     }
     cp_async_wait<0>();
 }
@@ -374,20 +404,16 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
     __shared__ __align__(16) float weights[2][kD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane / kLanes, part = lane % kLanes;
     const RopeColumns<kAdjacent> col(p.rot, part);
+    __shared__ RopeKind table[3];
+    rope_stage_kinds(p, table);
     long long begin, end;
     rope_share(p, begin, end);
-    RopeStream<kRows, 2> stream;
     const int mine = (int)(end - begin);
-    stream.left = mine;
-    stream.token = (int)rope_div(begin, p.groups);
-    stream.g = (int)(begin - (long long)stream.token * p.groups);
-    stream.row = row;
-    stream.lane_col = 8 * part;
-    stream.seg.n = 0;
-    int token = stream.token, g = stream.g;
+    RopePlace at(p, begin);
+    RopeStream<kRows, 2> stream(at, mine, row, 8 * part, 2);
     const uint32_t ring = ptx::smem_u32(u_s.rings[warp]) + 16 * lane;
 #pragma unroll 1
-    for (int i = 0; i < kRopeBackwardDepth; ++i) stream.ask(p, ring + 1024 * kRopeTwice * i);
+    for (int i = 0; i < kRopeBackwardDepth; ++i) stream.ask(p, table, ring + 1024 * kRopeTwice * i);
     rope_stage_weights<kD, kBf16, kAdjacent>(p, weights);
     int slot = 0, have_token = -1;
     const ptx::f32x2 zero = ptx::pack_f32x2(0.f, 0.f);
@@ -395,28 +421,28 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
     ptx::f32x2 cs[2] = {zero, zero}, sn[2] = {zero, zero};
 #pragma unroll 1
     for (int left = mine; left > 0;) {
-        RopeSegment seg = rope_segment<kRows>(p, token, g, left, row);
-        left -= seg.n;
-        if (token != have_token) {
-            have_token = token;
-            rope_angles(p, token, turns[warp]);
+        const RopeKind& kind = table[at.kind];
+        int n, first, rows_left;
+        rope_segment<kRows>(kind, at.from, left, row, n, first, rows_left);
+        left -= n;
+        if (at.token != have_token) {
+            have_token = at.token;
+            rope_angles(p, at.token, turns[warp]);
             if (col.turns) {
                 const float4 t0 = *reinterpret_cast<const float4*>(&turns[warp][4 * part]), t1 = *reinterpret_cast<const float4*>(&turns[warp][4 * part + 2]);
                 cs[0] = ptx::pack_f32x2(t0.x, t0.z); cs[1] = ptx::pack_f32x2(t1.x, t1.z);
                 sn[0] = ptx::pack_f32x2(t0.y, t0.w); sn[1] = ptx::pack_f32x2(t1.y, t1.w);
             }
         }
-        g += seg.n;
-        if (g == p.groups) { g = 0; ++token; }
-        const bool is_q = seg.kind == 0;
-        const int out_head = is_q ? p.q_out.head : p.k_out.head, out_half = out_head * kRows;
-        uint16_t* out = (is_q ? p.q_out.p : p.k_out.p) + (long long)seg.token * (is_q ? p.q_out.token : p.k_out.token) + (long long)seg.first * out_head + col.c0;
+        const bool is_q = at.kind == 0;
+        const int out_half = kind.out_head * kRows;
+        uint16_t* out = kind.out + (long long)at.token * kind.out_token + (long long)first * kind.out_head + col.c0;
         const bool normed = (is_q ? p.q_weight : p.k_weight) != nullptr;
-        const float4 wu4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part]), wv4 = *reinterpret_cast<const float4*>(&weights[seg.kind][8 * part + 4]);
+        const float4 wu4 = *reinterpret_cast<const float4*>(&weights[at.kind][8 * part]), wv4 = *reinterpret_cast<const float4*>(&weights[at.kind][8 * part + 4]);
         const ptx::f32x2 wu[2] = {ptx::pack_f32x2(wu4.x, wu4.y), ptx::pack_f32x2(wu4.z, wu4.w)}, wv[2] = {ptx::pack_f32x2(wv4.x, wv4.y), ptx::pack_f32x2(wv4.z, wv4.w)};
         ptx::f32x2 sum[4] = {zero, zero, zero, zero};      // of this segment: dn x r
 #pragma unroll 1
-        for (int i = 0; i < seg.n; ++i) {
+        for (int i = 0; i < n; ++i) {
             cp_async_wait<kRopeBackwardDepth - 1>();
             __syncwarp();
             uint4 in[kRopeTwice], grad[kRopeTwice];
@@ -426,7 +452,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
                 grad[h] = col.load(reinterpret_cast<const uint16_t*>(&u_s.rings[warp][slot][512 * (kRopeTwice + h) + 2 * kD * row]));
             }
             __syncwarp();
-            stream.ask(p, ring + 1024 * kRopeTwice * slot);
+            stream.ask(p, table, ring + 1024 * kRopeTwice * slot);
             slot = slot + 1 == kRopeBackwardDepth ? 0 : slot + 1;
 #pragma unroll
             for (int h = 0; h < kRopeTwice; ++h) {
@@ -440,7 +466,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
                         v[j] = ptx::sub2(ptx::mul2(v[j], cs[j]), su);
                     }
                 }
-                const bool there = seg.rows_left > h * kRows;
+                const bool there = rows_left > h * kRows;
                 if (normed) {
                     rope_unpack<kBf16, kAdjacent>(in[h], x, y);
                     const ptx::f32x2 gu[2] = {ptx::mul2(u[0], wu[0]), ptx::mul2(u[1], wu[1])}, gv[2] = {ptx::mul2(v[0], wv[0]), ptx::mul2(v[1], wv[1])};
@@ -462,13 +488,14 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
                 if (there) col.store_at(out + h * out_half, rope_pack<kBf16, kAdjacent>(u, v));
             }
             out += kRopeTwice * out_half;
-            seg.rows_left -= kRows * kRopeTwice;
+            rows_left -= kRows * kRopeTwice;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (is_q) dw[0][j] = ptx::add2(dw[0][j], sum[j]);
             else dw[1][j] = ptx::add2(dw[1][j], sum[j]);
         }
+        at.next(2);
     }
     cp_async_wait<0>();
     float (*sums)[kD] = u_s.sums;
