@@ -505,7 +505,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
 
 // Joins cut results: o = sum_i f_i o_i / sum_i f_i l_i over their parts, f_i = 2^(m_i - max m).  The n CTAs that hold the parts of a result
 // share its rows, so that a result cut into many parts has many hands.  (Left to the last CTA of a result to finish, with flags in place of
-// the second launch, one request of 131072 tokens took 92.8 us instead of 86.9, with one K/V head 315 instead of 34.)  A CTA has rows of at most two results; its eight warps take
+// the second launch, one request of 131072 tokens took 92.8 us instead of 86.9, with one K/V head 315 instead of 34.)  A CTA has rows
+// of at most two results; its eight warps take
 // one each, or where there are fewer than eight rows, as many to a row as there are, which take the parts in turn and
 // add up in a fixed order.
 // (Three CTAs' worth of registers, so that one fits where one of the decode's CTAs has ended: 64 requests of up to 500 tokens 21.0 us, with as

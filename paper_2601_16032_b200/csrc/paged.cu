@@ -17,6 +17,7 @@ using namespace sawtooth;
 
 constexpr int kMaxPageSize = 65536;
 constexpr int kMaxHeads = 65536;
+constexpr long long kMaxTokens = 2147483648ll - 128;   // of a request, for the decode
 constexpr int kRopeMaxCtas = 1024;     // of the backward pass; its workspace holds a partial sum of each
 // The backward pass runs as one cluster while each of its warps has few row groups.  (One launch instead of two saves the
 // host 2.4 us; on the GPU 60 row groups take 5.1 us against 5.4, 130 take 6.1 against 5.5, 260 take 8.2.)
@@ -290,7 +291,8 @@ int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* add
     if (pool->width < 1 || pool->capacity < 0) return fail(ATTN_ERR_INVALID_ARG, "width must be positive and capacity not negative");
     if ((long long)pool->width * pool->page_size > 2147483647ll || (long long)pool->width * B > 2147483647ll)
         return fail(ATTN_ERR_INVALID_ARG, "width * page_size and width * B must be below 2^31");
-    if (pool->table_stride < pool->width) return fail(ATTN_ERR_INVALID_ARG, "table_stride must be at least width");
+    if (pool->table_stride < pool->width || !fits_address(pool->table_stride, B))
+        return fail(ATTN_ERR_INVALID_ARG, "table_stride must be at least width, and not reach too far");
     if (((uintptr_t)cached | (uintptr_t)added | (uintptr_t)seq_len | (uintptr_t)q_start | (uintptr_t)position | (uintptr_t)request | (uintptr_t)info |
          (uintptr_t)pool->block_table | (uintptr_t)pool->free_pages | (uintptr_t)pool->free_count | (uintptr_t)pool->free_count_out) & 3u ||
         (uintptr_t)slot & 7u)
@@ -459,7 +461,7 @@ int attn_decode_query_plan(int B, int H, int kv_heads, int d, long long max_toke
     out->head_blocks = (H / kv_heads + rows - 1) / rows;
     out->min_tiles = kDecodeMinTiles;
     if (max_tokens < 0) return fail(ATTN_ERR_INVALID_ARG, "max_tokens must not be negative");
-    out->cluster = max_tokens == 0 ? 0 : decode_cluster((long long)B * kv_heads * out->head_blocks, max_tokens < 2147483647ll ? (int)max_tokens : 2147483647, decode_tile(d), out->grid);
+    out->cluster = max_tokens == 0 ? 0 : decode_cluster((long long)B * kv_heads * out->head_blocks, (int)(max_tokens < kMaxTokens ? max_tokens : kMaxTokens), decode_tile(d), out->grid);
     out->workspace_bytes = decode_workspace(out->grid, rows, d);
     return ATTN_OK;
 }
@@ -536,7 +538,8 @@ int attn_decode_paged(const void* q, const attn_kv_cache* cache, const int* bloc
     const int grid = decode_grid(ds.sm_count, z);
     const int rows = decode_rows(H / c.kv_heads), group = H / c.kv_heads;
     // (The kernel counts a CTA's tiles in 31 bits and the tiles of all CTAs, times their number, in 64.)
-    const long long room = (long long)max_pages * c.page_size, most = room < 2147483647ll ? room : 2147483647ll;
+    // (Below 2^31 by a tile, so that the last tile's token numbers do not pass 2^31.)
+    const long long room = (long long)max_pages * c.page_size, most = room < kMaxTokens ? room : kMaxTokens;
     if ((double)B * c.kv_heads * ((group + rows - 1) / rows) * ((double)most / decode_tile(c.d) + 1) > 1073741824.0 * grid)
         return fail(ATTN_ERR_INVALID_ARG, "B, kv_heads and max_pages * page_size allow more work than a call can count");
     const size_t need = decode_workspace(grid, rows, c.d);

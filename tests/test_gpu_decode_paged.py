@@ -240,6 +240,29 @@ def test_lengths_out_of_range_are_cut_and_reported():
     assert torch.equal(o[:2], want[:2]) and (o[2] == 0).all() and torch.isneginf(lse[2]).all()
 
 
+def test_the_longest_length():
+    """2^31 - 1 tokens, cut to the most there can be: one page again and again, so the result is that of the page alone."""
+    import math
+
+    import torch
+    import paper_2601_16032_b200 as sa
+    page, d = 65536, 64
+    k, v = (torch.randn((1, page, 1, d), device=DEV).bfloat16() for _ in range(2))
+    q = torch.randn((1, 2, d), device=DEV).bfloat16()
+    table = torch.zeros((1, 32768), dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([page], dtype=torch.int32, device=DEV)
+    want, want_lse = sa.decode_paged(q, k, v, table, lengths, return_lse=True)
+    sa.attn_device_status()
+    lengths.fill_(2**31 - 1)
+    o, lse = sa.decode_paged(q, k, v, table, lengths, return_lse=True)
+    with pytest.raises(sa.AttnError) as e:
+        sa.attn_device_status()
+    assert e.value.status == -7
+    # a thread's sums have 2^31 / (444 * 4 * 8) terms, each addition off by 2^-24 of the sum: 2^-6.7 at most
+    assert (lse - want_lse - math.log(32768)).abs().max() <= 1e-2
+    assert (o.float() - want.float()).abs().max() <= 1e-2 * v.float().abs().max()
+
+
 def test_workspace_contents_do_not_matter_and_its_end_is_kept():
     import torch
     import paper_2601_16032_b200 as sa

@@ -38,7 +38,7 @@ def plan_call(**change):
 @pytest.mark.parametrize("change,status", [
     (dict(table=0), -1), (dict(free=0), -1), (dict(count=0), -1), (dict(count_out=0), -1), (dict(cached=0), -1), (dict(added=0), -1), (dict(seq_len=0), -1),
     (dict(q_start=0), -1), (dict(slot=0), -1), (dict(info=0), -1), (dict(B=0), -1), (dict(B=8193), -1), (dict(cap=-1), -1), (dict(page=0), -1),
-    (dict(page=65537), -1), (dict(width=0), -1), (dict(capacity=-1), -1), (dict(stride=9), -1), (dict(width=1 << 28, stride=1 << 28), -1),
+    (dict(page=65537), -1), (dict(width=0), -1), (dict(capacity=-1), -1), (dict(stride=9), -1), (dict(stride=1 << 60), -1), (dict(width=1 << 28, stride=1 << 28), -1),
     (dict(cached=at(4) + 2), -3), (dict(slot=at(8) + 4), -3), (dict(position=at(9) + 1), -3),
     (dict(seq_len=at(4) + 4), -1), (dict(seq_len=at(5)), -1), (dict(position=at(10)), -1), (dict(info=at(1) + 4), -1), (dict(count_out=at(0) + 4 * 39), -1),
     (dict(slot=at(0)), -1), (dict(q_start=at(2) - 16), -1)])
