@@ -49,7 +49,7 @@ def _torch_commands(obj: str) -> tuple:
     includes = [f"-I{d}" for d in cpp_extension.include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]]
     libraries = [f"-L{d}" for d in cpp_extension.library_paths()]
     return ([cxx, "-std=c++17", "-O2", "-fPIC", "-DTORCH_EXTENSION_NAME=_torch_binding"] + includes + ["-c", "-o", obj, os.path.join(CSRC, TORCH_SOURCE)],
-            [cxx, "-shared", "-o", TORCH_LIB, obj] + libraries + ["-L" + PKG, "-lsawtooth_attn", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch",
+            [cxx, "-shared", "-o", TORCH_LIB, obj] + libraries + ["-L" + PKG, "-lsawtooth_attn", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch",
                                                                     "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
 
 

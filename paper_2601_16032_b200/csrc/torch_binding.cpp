@@ -4,6 +4,7 @@
 // Compiled, unlike the ctypes binding of the attention calls: these calls run for a few microseconds on the GPU and take
 // many small tensors, so what Python spends on looking each of them over would take several times as long as they do
 // (attn_page_plan: 31 us a call through ctypes and Python checks).  There is one path: without this module the wrappers raise.
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/extension.h>
@@ -43,11 +44,16 @@ int kind_of(const Tensor& t) {
     return ATTN_F16;
 }
 
+// A new tensor on `like`'s device, without the way through the dispatcher.
+Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const Tensor& like) {
+    return Tensor(at::detail::empty_cuda(sizes, type, like.device(), std::nullopt));
+}
+
 // Tensors of one dimension cut from one allocation: a caching allocator's call takes longer than all else that a small
 // output costs.  Each starts on a multiple of 16 bytes.
 class Cuts {
 public:
-    Cuts(int64_t bytes, const Tensor& like) : base_(at::empty({bytes}, like.options().dtype(at::kByte))) {}
+    Cuts(int64_t bytes, const Tensor& like) : base_(fresh({bytes}, at::kByte, like)) {}
     static int64_t room(int64_t n, int64_t size) { return (n * size + 15) / 16 * 16; }
     Tensor take(int64_t n, at::ScalarType type) {
         const int64_t size = (int64_t)c10::elementSize(type);
@@ -179,9 +185,9 @@ py::tuple qk_norm_rope(const Tensor& q, const Tensor& k, const OptTensor& v, con
     need(v_cache.has_value() == cached && slot.has_value() == cached && v.has_value() == cached, "k_cache, v_cache, slot and v go together");
     const c10::cuda::OptionalCUDAGuard guard(q.device());
     const RopeArgs a(q, q_weight, k_weight, position, inv_freq);
-    Tensor q_out = q_out_given ? *q_out_given : at::empty(q.sizes(), q.options());
+    Tensor q_out = q_out_given ? *q_out_given : fresh(q.sizes(), q.scalar_type(), q);
     OptTensor k_out = k_out_given;
-    if (!k_out && !cached) k_out = at::empty(k.sizes(), k.options());
+    if (!k_out && !cached) k_out = fresh(k.sizes(), k.scalar_type(), k);
     need(q_out.sizes() == q.sizes() && (!k_out || k_out->sizes() == k.sizes()) && (!v || v->sizes() == k.sizes()), "v, q_out and k_out must have the shapes of k, q and k");
     attn_rope_opts o = {};
     const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), rk = rows_of(k, q, "k must be like q: type, device, rows of d contiguous elements"),
@@ -207,7 +213,7 @@ py::tuple qk_norm_rope(const Tensor& q, const Tensor& k, const OptTensor& v, con
 
 // The caller's workspace, or a new one; its size is checked by the C ABI.
 Tensor workspace_of(const OptTensor& given, size_t bytes, const Tensor& like) {
-    if (!given) return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+    if (!given) return fresh({(int64_t)bytes}, at::kByte, like);
     need(given->device() == like.device() && given->is_contiguous(), "the workspace must be a contiguous tensor on q's device");
     return *given;
 }
@@ -218,7 +224,7 @@ py::tuple qk_norm_rope_backward(const Tensor& dq_out, const Tensor& dk_out, cons
     check_qk(q, k);
     const c10::cuda::OptionalCUDAGuard guard(q.device());
     const RopeArgs a(q, q_weight, k_weight, position, inv_freq);
-    Tensor dq = dq_given ? *dq_given : at::empty(q.sizes(), q.options()), dk = dk_given ? *dk_given : at::empty(k.sizes(), k.options());
+    Tensor dq = dq_given ? *dq_given : fresh(q.sizes(), q.scalar_type(), q), dk = dk_given ? *dk_given : fresh(k.sizes(), k.scalar_type(), k);
     need(dq.sizes() == q.sizes() && dq_out.sizes() == q.sizes() && dk.sizes() == k.sizes() && dk_out.sizes() == k.sizes(), "gradients must have the shapes of q and k");
     OptTensor dq_weight, dk_weight;
     if (a.q_weight || a.k_weight) {
@@ -257,10 +263,10 @@ py::tuple decode_paged(const Tensor& q, const Tensor& k_cache, const Tensor& v_c
     need(table.dim() == 2 && table.scalar_type() == at::kInt && table.device() == q.device() && table.size(0) == B && table.size(1) > 0 &&
              table.size(1) <= 2147483647 && (table.size(1) == 1 || table.stride(1) == 1),
          "block_table must be an int32 tensor [B, max_pages] on q's device with contiguous rows");
-    Tensor o = out ? *out : at::empty(q.sizes(), q.options());
+    Tensor o = out ? *out : fresh(q.sizes(), q.scalar_type(), q);
     need(o.sizes() == q.sizes(), "out must have q's shape");
     OptTensor lse;
-    if (return_lse) lse = at::empty({B, H}, q.options().dtype(at::kFloat));
+    if (return_lse) lse = fresh({B, H}, at::kFloat, q);
     if (B == 0) return py::make_tuple(o, lse);
     const attn_kv_cache cache = cache_of(k_cache, v_cache, layout, -1, d, q);
     const Rows rq = rows_of(q, q, "q: rows of d contiguous elements"), ro = rows_of(o, q, "out must be like q: type, device, rows of d contiguous elements");
