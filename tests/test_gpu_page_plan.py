@@ -68,6 +68,19 @@ def test_most_requests():
     run_and_compare(step[0], step[1], 16, *step[2:], 9000)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,page,longest,leaving", [(700, 1, 1500, 400), (1, 1, 200000, 1), (40, 3, 5000, 40)])
+def test_many_pages_given_back(B, page, longest, leaving, in_place):
+    """More pages return to the stack than there are threads, and a request's many pages alone."""
+    rng = np.random.default_rng(11)
+    cached, added, table, free, count = random_step(rng, B, page, longest, leaving=leaving)
+    if B == 1:   # the request holds all pages
+        cached[0], held = longest, paged.pages_of(longest, page)
+        table = rng.permutation(held + 7)[:table.shape[1]].astype(np.int32)[None]
+        free, count = np.full(held + 7, -5, dtype=np.int32), 0
+    run_and_compare(cached, added, page, table, free, count, int(np.maximum(added, 0).sum()) + 2, in_place=in_place)
+
+
 @pytest.mark.parametrize("change,state", [
     (dict(cached=-1), 1), (dict(added=-2), 1), (dict(cached=10**6), 1), (dict(added=2**31 - 1), 1), (dict(count=-1), 1), (dict(count=10**6), 1),
     (dict(cap=0), 2), (dict(count=0), 3)])
