@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kN) : "memory");
     };
 
+    previous_kernel_wait();
     DecodeCursor<G::kTile> ld;
     int left;                        // tiles of this CTA's share
     int joins = 0;                   // bit i: entry 2 cta + i of p.join is written
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) decode_join_kernel(const Deco
     __shared__ float sums[kWarps][kD];
     __shared__ float2 sums_ml[kWarps];
     const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, block_rows = decode_rows(p.group);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    previous_kernel_wait();
     const int4 joins[2] = {p.join[2 * cta], p.join[2 * cta + 1]};
     // Of a result with n parts from CTA c0 on, this CTA takes rows cta - c0, cta - c0 + n, ...
     auto rows_of = [&](const int4& j) { return min(block_rows, p.group - (j.w % p.head_blocks) * block_rows); };

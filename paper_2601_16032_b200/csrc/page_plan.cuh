@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(1024) page_plan_kernel(const PagePlanParams p)
     const int rank = blockIdx.x, everyone = gridDim.x * threads;
     const unsigned full = 0xffffffffu;
 
+    previous_kernel_wait();
     const int count = *p.free_count;
     int tokens = 0, taken = 0, given = 0;      // totals so far
     long long tokens64 = 0;

@@ -65,13 +65,13 @@ int launch_status(cudaError_t e) {
     return fail(ATTN_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
-// cudaLaunchKernelEx with a cluster of `cluster` CTAs (0: none) and, with `after`, the early launch behind the previous kernel
-// of the stream, which the kernel itself waits for.
+// cudaLaunchKernelEx with a cluster of `cluster` CTAs (0: none), launched early behind the previous kernel of the stream, which the kernel
+// itself waits for (previous_kernel_wait).  (Calls one after another on a stream, against launches in order: rotation of 4001 tokens at d = 64
+// 14.5 -> 12.7 us, its gradient of 8192 at d = 128 49.0 -> 46.2, decode of one request of 1000 tokens 8.4 -> 6.7, of 131072 90.6 -> 88.4.)
 template <typename... Params, typename... Args>
-cudaError_t launch_ex(void (*kernel)(Params...), int grid_x, int grid_y, int threads, size_t smem, cudaStream_t stream, int cluster, bool after,
-                      Args... args) {
+cudaError_t launch_ex(void (*kernel)(Params...), int grid, int threads, size_t smem, cudaStream_t stream, int cluster, Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid_x, (unsigned)grid_y);
+    cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -83,11 +83,9 @@ cudaError_t launch_ex(void (*kernel)(Params...), int grid_x, int grid_y, int thr
         attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
         ++n;
     }
-    if (after) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n].val.programmaticStreamSerializationAllowed = 1;
-        ++n;
-    }
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
     cfg.attrs = attr;
     cfg.numAttrs = (unsigned)n;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
@@ -241,7 +239,7 @@ int launch_decode_form(int dev, const DeviceState& ds, const DecodeParams& p, in
     constexpr int kSmem = DecodeGeometry<kD>::kSmem, kBit = kRaisedDecode + ((kD == 128) * 4 + kBf16 * 2 + kCluster) * 3 + kN / 2;
     DecodeKernel kernel = decode_paged_kernel<kD, kBf16, kN, kCluster>;
     int rc = raise_smem(dev, ds, (const void*)kernel, kBit, kSmem);
-    return rc ? rc : launch_status(launch_ex(kernel, grid, 1, kDecodeThreads, kSmem, st, kCluster ? p.cluster : 0, false, p));
+    return rc ? rc : launch_status(launch_ex(kernel, grid, kDecodeThreads, kSmem, st, kCluster ? p.cluster : 0, p));
 }
 template <int kD, int kBf16, bool kCluster>
 int launch_decode_rows(int dev, const DeviceState& ds, const DecodeParams& p, int grid, cudaStream_t st) {
@@ -255,7 +253,7 @@ int launch_decode(int dev, const DeviceState& ds, DecodeParams& p, int grid, cud
     p.cluster = decode_cluster(results, p.max_len, decode_tile(kD), grid);
     if (p.cluster) return launch_decode_rows<kD, kBf16, true>(dev, ds, p, (int)(results * p.cluster), st);
     int rc = launch_decode_rows<kD, kBf16, false>(dev, ds, p, grid, st);
-    return rc ? rc : launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, 1, kJoinThreads, 0, st, 0, true, p));
+    return rc ? rc : launch_status(launch_ex(DecodeKernel(decode_join_kernel<kD, kBf16>), grid, kJoinThreads, 0, st, 0, p));
 }
 
 size_t decode_workspace(int grid, int rows, int d) {
@@ -333,7 +331,7 @@ int attn_page_plan(const attn_page_pool* pool, const int* cached, const int* add
     const int threads = p.in_place && items > 512 ? 1024 : items <= 256 ? 256 : 512;
     const long long want = (items + threads - 1) / threads;
     const int ctas = p.in_place ? (want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8) : (int)std::min(want, 2ll * ds.sm_count);
-    return launch_status(launch_ex(page_plan_kernel, ctas, 1, threads, smem, static_cast<cudaStream_t>(stream), p.in_place ? ctas : 0, false, p));
+    return launch_status(launch_ex(page_plan_kernel, ctas, threads, smem, static_cast<cudaStream_t>(stream), p.in_place ? ctas : 0, p));
 }
 
 int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out, int T, int H, int kv_heads, int d, int dtype,
@@ -381,8 +379,7 @@ int attn_qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, 
     if (z.cache) p.v = in_of(rv);
     rope_groups(&p, d, z.cache != nullptr);
     const int grid = rope_grid(p, kRopeForwardCtas * ds.sm_count);
-    rope_kernel(d, dtype, rot_style, false)<<<grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    if ((rc = launch_status(cudaGetLastError()))) return rc;
+    if ((rc = launch_status(launch_ex(rope_kernel(d, dtype, rot_style, false), grid, kRopeThreads, 0, static_cast<cudaStream_t>(stream), 0, p)))) return rc;
     return z.check_mode ? read_status(nullptr) : ATTN_OK;
 }
 
@@ -430,16 +427,15 @@ int attn_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
         p.dk_weight = dk_weight;
         const long long need = ((long long)T * p.groups + kRopeWarps - 1) / kRopeWarps;
         const int ctas = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : kRopeCluster;
-        rc = launch_status(launch_ex(rope_kernel(d, dtype, rot_style, true), ctas, 1, kRopeThreads, 0, st, ctas, false, p));
+        rc = launch_status(launch_ex(rope_kernel(d, dtype, rot_style, true), ctas, kRopeThreads, 0, st, ctas, p));
         if (rc) return rc;
         return z.check_mode ? read_status(nullptr) : ATTN_OK;
     }
     p.partial = static_cast<float*>(workspace);
     const int grid = rope_grid(p, kRopeBackwardCtas * ds.sm_count < kRopeMaxCtas ? kRopeBackwardCtas * ds.sm_count : kRopeMaxCtas);
-    rope_kernel(d, dtype, rot_style, true)<<<grid, kRopeThreads, 0, st>>>(p);
-    if ((rc = launch_status(cudaGetLastError()))) return rc;
+    if ((rc = launch_status(launch_ex(rope_kernel(d, dtype, rot_style, true), grid, kRopeThreads, 0, st, 0, p)))) return rc;
     if (dq_weight || dk_weight) {
-        rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 8, 1, 1024, 0, st, 0, true, (const float*)p.partial, grid, d, dq_weight, dk_weight));
+        rc = launch_status(launch_ex(rope_weight_sum_kernel, 2 * d / 8, 1024, 0, st, 0, (const float*)p.partial, grid, d, dq_weight, dk_weight));
         if (rc) return rc;
     }
     return z.check_mode ? read_status(nullptr) : ATTN_OK;

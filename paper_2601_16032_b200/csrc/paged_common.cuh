@@ -36,6 +36,10 @@ struct CacheView {
 
 __device__ __forceinline__ void note_index(int* status, int code) { atomicCAS(status, 0, code); }
 
+// The kernels here are launched before the previous one of the stream has ended.  Until all that it wrote can be seen no thread reads or
+// writes global memory, and since every thread waits, a kernel that has ended leaves none behind it that still runs.
+__device__ __forceinline__ void previous_kernel_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes)   // copies `bytes` (16 or 0), zero-fills the rest
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");

@@ -281,6 +281,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeForwardCtas) qk_norm_rope_k
     const RopeColumns<kAdjacent> col(p.rot, part);
     __shared__ RopeKind table[3];
     rope_stage_kinds(p, table);
+    previous_kernel_wait();
     long long begin, end;
     rope_share(p, begin, end);
     const int mine = (int)(end - begin), kinds = p.slot ? 3 : 2;
@@ -406,6 +407,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
     const RopeColumns<kAdjacent> col(p.rot, part);
     __shared__ RopeKind table[3];
     rope_stage_kinds(p, table);
+    previous_kernel_wait();
     long long begin, end;
     rope_share(p, begin, end);
     const int mine = (int)(end - begin);
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeBackwardCtas) qk_norm_rope_
 __global__ void __launch_bounds__(1024) rope_weight_sum_kernel(const float* partial, int ctas, int d, float* dq_weight, float* dk_weight)
 {
     __shared__ float sums[32][8];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    previous_kernel_wait();
     const int col = threadIdx.x & 7, row = threadIdx.x >> 3, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, column = blockIdx.x * 8 + col;   // of 2 d
     float a = 0.f;
 #pragma unroll 4

@@ -1,7 +1,8 @@
 """The entry points around the paged key/value cache for torch CUDA tensors.
 
 Like `forward` they only check and marshal, in the compiled module _torch_binding (csrc/torch_binding.cpp): shapes, strides, pointers
-and the current stream of the tensors' device go to the C ABI.  Outputs that are not given are allocated with torch.
+and the current stream of the tensors' device go to the C ABI.  Outputs that are not given are allocated with torch.  Nothing is recorded
+for autograd: a training step calls qk_norm_rope_backward itself.
 """
 from __future__ import annotations
 

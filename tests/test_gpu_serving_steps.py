@@ -186,3 +186,113 @@ def test_a_captured_decode_step():
     for turn, (a, b) in enumerate(zip(*outs)):
         if turn >= 20 and turn % 2:
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def _step_calls():
+    """(name, inputs, call): each call's results depend on its inputs alone; pairs of calls share a workspace."""
+    import torch
+    import paper_2601_16032_b200 as sa
+    torch.manual_seed(9)
+    bf = torch.bfloat16
+    made = []
+
+    def rope(tokens, H, Hk, d, backward):
+        q, k, gq, gk = (torch.randn(tokens, h, d, device=DEV).to(bf) for h in (H, Hk, H, Hk))
+        w = torch.randn(d, device=DEV).to(bf)
+        freq = (1e4 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).to(DEV)
+        position = torch.arange(tokens, dtype=torch.int32, device=DEV)
+        work = torch.empty(sa.attn_rope_bwd_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+        common = dict(q_weight=w, k_weight=w, position=position, inv_freq=freq)
+        if backward:
+            return [q, k, gq, gk], lambda: sa.qk_norm_rope_backward(gq, gk, q, k, workspace=work, **common)
+        return [q, k, position], lambda: sa.qk_norm_rope(q, k, **common)
+
+    def decode(B, longest, H, Hk, d):
+        page = 16
+        width = -(-longest // page)
+        kc, vc = (torch.randn(B * width, page, Hk, d, device=DEV).to(bf) for _ in range(2))
+        table = torch.arange(B * width, dtype=torch.int32, device=DEV).view(B, width)
+        q = torch.randn(B, H, d, device=DEV).to(bf)
+        length = torch.randint(1, longest + 1, (B,), device=DEV).to(torch.int32)
+        work = torch.empty(sa.attn_decode_query_plan(B, H, Hk, d).workspace_bytes, dtype=torch.uint8, device=DEV)
+        return [q, kc, vc, length], lambda: sa.decode_paged(q, kc, vc, table, length, return_lse=True, workspace=work)
+
+    def plan(B):
+        i32 = dict(dtype=torch.int32, device=DEV)
+        cached, added = torch.randint(0, 50, (B,), **i32), torch.randint(0, 3, (B,), **i32)
+        table, free = torch.arange(B * 8, **i32).view(B, 8), torch.arange(B * 8, B * 12, **i32)
+        count = torch.tensor([B * 4], **i32)
+        return [cached, added, table, free, count], lambda: sa.page_plan(cached, added, 16, table, free, count, 2 * B)
+
+    for name, (inputs, call) in dict(plan=plan(300), rope=rope(700, 8, 2, 64, False), rope_bwd=rope(700, 8, 2, 64, True), rope_bwd_small=rope(5, 4, 2, 128, True),
+                                     decode=decode(30, 2000, 8, 2, 128), decode_short=decode(4, 200, 8, 2, 64)).items():
+        made.append((name, inputs, call))
+    return made
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("before", ["kernel", "copy", "other stream"])
+def test_steps_wait_for_what_comes_before_them(before, captured):
+    """The kernels start behind one that has not ended: inputs that a late kernel, a copy or another stream writes, overwritten again behind
+    the call, and a second call with other inputs in the same workspace."""
+    import torch
+    busy = torch.randn(3000, 3000, device=DEV)
+    for name, inputs, call in _step_calls():
+        good = [[t.clone() for t in inputs]]
+        # The second inputs: rows in another order (lengths and positions stay within what their tables hold).
+        good.append([t.clone() if name == "plan" else t.flip(0).contiguous() for t in inputs])
+        want = []
+        for g in good:
+            for t, x in zip(inputs, g):
+                t.copy_(x)
+            torch.cuda.synchronize()
+            want.append([o.clone() for o in call() if o is not None] + ([inputs[2].clone(), inputs[3].clone()] if name == "plan" else []))
+            torch.cuda.synchronize()
+        got = []
+
+        def late():
+            y = busy
+            for _ in range(4):
+                y = torch.sin(y) @ busy
+            return y
+
+        def run():
+            got.clear()
+            main, side = torch.cuda.current_stream(), torch.cuda.Stream()
+            for g in good:
+                if before == "other stream":
+                    side.wait_stream(main)
+                    with torch.cuda.stream(side):
+                        late()
+                        for t, x in zip(inputs, g):
+                            t.copy_(x)
+                    main.wait_stream(side)
+                else:
+                    late()
+                    for t, x in zip(inputs, g):
+                        if before == "copy":
+                            t.copy_(x)
+                        else:
+                            torch.add(x, 0, out=t)
+                out = [o for o in call() if o is not None] + ([inputs[2].clone(), inputs[3].clone()] if name == "plan" else [])
+                for t in inputs:
+                    t.zero_()
+                got.append(out)
+
+        if captured:
+            warm = torch.cuda.Stream()
+            warm.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(warm):
+                run()
+            torch.cuda.current_stream().wait_stream(warm)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                run()
+            for _ in range(3):
+                graph.replay()
+        else:
+            run()
+        torch.cuda.synchronize()
+        for turn in range(2):
+            for i, (a, b) in enumerate(zip(got[turn], want[turn])):
+                assert torch.equal(a.view(torch.uint8) if a.dim() else a, b.view(torch.uint8) if b.dim() else b), (name, turn, i)
