@@ -135,7 +135,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kN) : "memory");
     };
 
-    previous_kernel_wait();
     DecodeCursor<G::kTile> ld;
     int left;                        // tiles of this CTA's share
     int joins = 0;                   // bit i: entry 2 cta + i of p.join is written
@@ -146,6 +145,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         const int result = cta / p.cluster, rank = cta % p.cluster;
         ld.b = result / blocks;
         ld.block = result % blocks;
+        previous_kernel_wait();
         const int raw = p.seq_len[ld.b];
         if (cta % (blocks * p.cluster) == 0 && tid == 0 && (raw < 0 || raw > p.max_len)) note_index(p.status, kIndexLength);
         ld.len = decode_cut(p, raw);
@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 3) decode_paged_kernel(const D
         const int chunk = (p.B + kDecodeThreads - 1) / kDecodeThreads, b_lo = min(p.B, tid * chunk), b_hi = min(p.B, b_lo + chunk);
         uint64_t mine = 0;
         bool bad = false;
+        previous_kernel_wait();
         for (int b = b_lo; b < b_hi; ++b) {
             const int raw = p.seq_len[b];
             bad |= raw < 0 || raw > p.max_len;
