@@ -1,7 +1,7 @@
 // Attention of one new token per request over a paged cache: one pass over K and V with a running maximum and sum, the work
 // split evenly over the CTAs along the lengths (decode_schedule.h), and a second, short kernel that joins what the split cut.
 // Measured, of the copy rate of 6.55 TB/s: 64 requests of up to 8192 tokens (32 / 8 heads, d = 128, bf16) 160 us, 96 %; 8 requests of
-// 131072 (16 heads, d = 64, fp16) 614 us, 107 % (reading alone is faster than copying); one of 131072 (32 / 8) 87.5 us, 94 %, of which the
+// 131072 (16 heads, d = 64, fp16) 614 us, 107 % (reading alone is faster than copying); one of 131072 (32 / 8) 87 us, 94 %, of which the
 // join takes 4.  Short requests are bound by the chain launch, lengths, page numbers, K and V, sums: 4.3 us at 64 tokens.
 //
 // What bounds it is reading K and V once: per K/V head and token 4 d bytes against 4 d multiply-adds per query head.  So
@@ -12,8 +12,9 @@
 // mma.sync m16n8k16 and query heads as its 8 columns, so that up to 8 heads cost half of what they would as rows.  Turning P
 // round between the products takes a movmatrix per 8 x 8 block.  A warp works for 8 heads; where 9 to 16 or 17 to 32 share a K/V head, two
 // or four warps form a group that pools its tokens: each reads all of them for its own 8 heads, which leaves fewer sums to add up
-// at the end of a request (none for four) and keeps every warp's chain of products short (200 requests of up to 700 tokens, 32 heads on one
-// K/V head: 22.3 us; with 16 heads a warp, which halves the reads of shared memory, 27.4).  A 128-row tcgen05 tile would be as
+// at the end of a request (none for four) and keeps every warp's chain of products short.  (32 heads on one K/V head: 10 requests of
+// up to 128111 tokens 77 us, 65 %, with 16 heads a warp, which halves the reads of shared memory, 83; 200 of up to 700 tokens 20.8 us, and 22.3
+// against 27.4 when that was measured.  Shared memory is then 60 % busy, the tensor pipe 43, issue 42: fixed latencies of 12 warps are left.)  A 128-row tcgen05 tile would be as
 // well filled in this form, but the products are not what bounds the kernel, and the way through tensor memory would add to the
 // latency of short calls.
 //
