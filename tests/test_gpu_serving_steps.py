@@ -231,7 +231,7 @@ def _step_calls():
 
 
 @pytest.mark.parametrize("captured", [False, True])
-@pytest.mark.parametrize("before", ["kernel", "copy", "other stream"])
+@pytest.mark.parametrize("before", ["kernel", "copy", "kernel on another stream", "copy on another stream"])
 def test_steps_wait_for_what_comes_before_them(before, captured):
     """The kernels start behind one that has not ended: inputs that a late kernel, a copy or another stream writes, overwritten again behind
     the call, and a second call with other inputs in the same workspace."""
@@ -260,20 +260,17 @@ def test_steps_wait_for_what_comes_before_them(before, captured):
             got.clear()
             main, side = torch.cuda.current_stream(), torch.cuda.Stream()
             for g in good:
-                if before == "other stream":
-                    side.wait_stream(main)
-                    with torch.cuda.stream(side):
-                        late()
-                        for t, x in zip(inputs, g):
-                            t.copy_(x)
-                    main.wait_stream(side)
-                else:
+                side.wait_stream(main)
+                with torch.cuda.stream(side if "another" in before else main):
                     late()
                     for t, x in zip(inputs, g):
-                        if before == "copy":
+                        if "copy" in before:
                             t.copy_(x)
                         else:
                             torch.add(x, 0, out=t)
+                main.wait_stream(side)
+                if "copy on another" in before:   # one more kernel between the wait and the call; behind a kernel none
+                    busy.add_(0)
                 out = [o for o in call() if o is not None] + ([inputs[2].clone(), inputs[3].clone()] if name == "plan" else [])
                 for t in inputs:
                     t.zero_()
